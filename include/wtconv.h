@@ -242,6 +242,167 @@ wtconv_status wtconv_backward_noalloc(const wtconv_desc* desc, const void* x, co
                                       float* const* d_level_w, float* const* d_level_scale,
                                       hipStream_t stream);
 
+/*
+ * Operators around the convolution in a network block, and the optimizer.
+ *
+ * A block runs convolution -> layer norm over the channels -> pointwise
+ * products -> scaled residual. The convolution works on planes, x[B][C][S]
+ * with S = H * W pixels, the products on rows, x[B][S][C]: the layer norm
+ * changes from the first to the second as it normalises, the residual changes
+ * back as it adds. The conventions above hold for these entry points too
+ * (caller's buffers, float32 parameters and sums, fixed order of every sum,
+ * argument errors before any HIP call), with these differences: B and S may be
+ * 0 (nothing is normalised or added, parameter gradients are zero), and
+ * pointers need only the alignment of their element type.
+ */
+#define WTCONV_MAX_CHANNELS (1 << 20)
+
+typedef enum {
+    WTCONV_ROWS = 0,  /* [B][S][C]: the channels of a pixel are adjacent           */
+    WTCONV_PLANES = 1 /* [B][C][S]: the pixels of a channel are adjacent           */
+} wtconv_layout;
+
+typedef struct {
+    long long B, S; /* images and pixels of an image, >= 0                       */
+    int C;          /* channels, 1 to WTCONV_MAX_CHANNELS                        */
+    wtconv_layout in, out; /* layout of x and dx, and of y and dy: ROWS -> ROWS,
+                              PLANES -> ROWS or PLANES -> PLANES                 */
+    long long x_stride, dy_stride; /* elements from one row of x or of dy to the
+                              next, >= C; 0 means C. Rows only: planes are dense,
+                              and so are y and dx                                */
+    double eps;     /* added to the variance, >= 0                               */
+    wtconv_dtype dtype;
+} wtconv_norm_desc;
+
+/*
+ * Layer norm over the channels of each pixel:
+ *   mean = sum_c x / C,  rstd = 1 / sqrt(sum_c (x - mean)^2 / C + eps),
+ *   y = (x - mean) * rstd * weight + bias.
+ *   x       B * S pixels of C channels, dtype, in the layout desc->in
+ *   weight, bias  [C] float32; NULL means ones, zeros
+ *   y       dtype, in the layout desc->out; must not overlap an input
+ *   mean, rstd    [B * S] float32, what the backward pass needs; both NULL
+ *           where there is none
+ */
+wtconv_status wtconv_layer_norm_forward(const wtconv_norm_desc* desc, const void* x, const float* weight,
+                                        const float* bias, void* y, float* mean, float* rstd,
+                                        hipStream_t stream);
+
+/* Bytes of device workspace wtconv_layer_norm_backward needs (0 on a bad desc). */
+size_t wtconv_layer_norm_backward_workspace_bytes(const wtconv_norm_desc* desc);
+
+/*
+ * Gradients of sum(y * dy). With xhat = (x - mean) * rstd and g = dy * weight:
+ *   dx = rstd * (g - mean_c(g) - xhat * mean_c(g * xhat)),
+ *   d_weight = sum over pixels of dy * xhat,  d_bias = sum over pixels of dy.
+ *   dy      dtype, in the layout desc->out
+ *   x, mean, rstd, weight  as the forward pass took and gave them
+ *   dx      dtype, in the layout desc->in, or NULL to skip it
+ *   d_weight, d_bias  [C] float32, or NULL to skip either
+ *   workspace  at least wtconv_layer_norm_backward_workspace_bytes(desc) bytes,
+ *           16-byte aligned
+ */
+wtconv_status wtconv_layer_norm_backward(const wtconv_norm_desc* desc, const void* dy, const void* x,
+                                         const float* mean, const float* rstd, const float* weight, void* dx,
+                                         float* d_weight, float* d_bias, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream);
+
+typedef struct {
+    long long B, S; /* images and pixels of an image, >= 0 */
+    int C;          /* channels, 1 to WTCONV_MAX_CHANNELS  */
+    wtconv_dtype dtype;
+} wtconv_residual_desc;
+
+/*
+ * Scaled residual, y[b][c][s] = x[b][c][s] + k[b] * gamma[c] * z[b][s][c].
+ *   x, y    planes, dtype;  z  rows, dtype
+ *   gamma   [C] float32, or NULL for ones
+ *   sample_scale  k, [B] float32 (0 for an image that drops its branch), or
+ *           NULL for ones
+ * y must not overlap an input.
+ */
+wtconv_status wtconv_scaled_residual_forward(const wtconv_residual_desc* desc, const void* x, const void* z,
+                                             const float* gamma, const float* sample_scale, void* y,
+                                             hipStream_t stream);
+
+/* Bytes of device workspace wtconv_scaled_residual_backward needs (0 on a bad desc). */
+size_t wtconv_scaled_residual_backward_workspace_bytes(const wtconv_residual_desc* desc);
+
+/*
+ * Gradients of sum(y * dy); the one of x is dy itself.
+ *   dz[b][s][c] = k[b] * gamma[c] * dy[b][c][s]  (rows, dtype; NULL to skip it)
+ *   d_gamma[c] = sum over b, s of k[b] * dy[b][c][s] * z[b][s][c]  ([C] float32;
+ *           NULL to skip it; z may then be NULL)
+ *   workspace  at least wtconv_scaled_residual_backward_workspace_bytes(desc)
+ *           bytes, 16-byte aligned
+ */
+wtconv_status wtconv_scaled_residual_backward(const wtconv_residual_desc* desc, const void* dy, const void* z,
+                                              const float* gamma, const float* sample_scale, void* dz,
+                                              float* d_gamma, void* workspace, size_t workspace_bytes,
+                                              hipStream_t stream);
+
+/*
+ * AdamW over many tensors at once. For step t of a tensor (the first is 1):
+ *   m = beta1 * m + (1 - beta1) * g,  v = beta2 * v + (1 - beta2) * g * g,
+ *   p = p * (1 - lr * weight_decay)
+ *       - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps),
+ * where g is the gradient, times grad_scale[0] if that is given.
+ *
+ * The moments m and v of a group's tensors lie in two buffers, each tensor's
+ * from its `offset` on, a multiple of 64 elements; a buffer holds the last
+ * tensor's elements rounded up to 64. state_bits = 32: float32. state_bits = 8:
+ * one byte for each element, and one scale byte for each 64 elements, in two
+ * buffers more. The scale is the biased exponent of the largest magnitude of
+ * its block, 255 if one is not finite (the block then stands for NaN). A code
+ * of m is a sign, 4 bits of exponent and 3 of mantissa, one of v 5 bits of
+ * exponent and 3 of mantissa: the float32 with these bits below its sign
+ * stands for itself times 2^(scale - 14) for m, 2^(scale - 30) for v, so that
+ * the block's largest has exponent field 14 or 30 and small values underflow
+ * gradually. A moment is rounded down or up at random, up with the probability
+ * of its place between the two codes (for beta2 = 0.999 a step changes v by
+ * less than half the distance between two codes, so that rounding to nearest
+ * would hold v where it is): 20 mantissa bits are dropped after 16 * r + 8 was
+ * added, with the low 16 bits r of a hash of `key` and of the element's place
+ * in the buffer for m, and the high 16 bits for v. The update of p takes the
+ * moments before this rounding.
+ */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay; /* lr, eps, weight_decay >= 0; 0 <= beta < 1 */
+    long long step;                             /* t of these tensors, >= 1                  */
+    unsigned key;                               /* of the random bits (8-bit moments)        */
+    void *exp_avg, *exp_avg_sq;                 /* buffers of m and v                        */
+    unsigned char *exp_avg_scale, *exp_avg_sq_scale; /* their scales (8-bit moments)         */
+} wtconv_adamw_group;
+
+typedef struct {
+    void* param;       /* numel elements of dtype                                          */
+    const void* grad;  /* numel elements of dtype, in the order of param                   */
+    long long numel;   /* >= 0                                                             */
+    long long offset;  /* of its moments in the group's buffers                            */
+    int group;         /* index into the groups                                            */
+} wtconv_adamw_tensor;
+
+/*
+ * One step of n_tensors tensors, in place. `groups` and `tensors` are host
+ * arrays, read before the call returns; the moment buffers are 16-byte aligned. grad_scale: device pointer to one
+ * float32, or NULL. No tensor, gradient or moment may overlap another. A
+ * hyperparameter outside its range, or a state_bits other than 8 and 32,
+ * returns WTCONV_ERR_UNSUPPORTED; an offset that is no multiple of 64 or a
+ * group that is not there WTCONV_ERR_SHAPE.
+ */
+wtconv_status wtconv_adamw_step(int n_groups, const wtconv_adamw_group* groups, int n_tensors,
+                                const wtconv_adamw_tensor* tensors, wtconv_dtype dtype, int state_bits,
+                                const float* grad_scale, hipStream_t stream);
+
+/*
+ * The values that n elements of 8-bit moments stand for (n a multiple of 64,
+ * from the start of a block), of m and v at once: m, v are n elements of
+ * dtype. bfloat16 holds every such value down to 2^-126 exactly.
+ */
+wtconv_status wtconv_adamw_moments(long long n, const unsigned char* exp_avg, const unsigned char* exp_avg_scale,
+                                   const unsigned char* exp_avg_sq, const unsigned char* exp_avg_sq_scale,
+                                   void* m, void* v, wtconv_dtype dtype, hipStream_t stream);
+
 /* Static, human-readable name of a status code. */
 const char* wtconv_status_string(wtconv_status status);
 

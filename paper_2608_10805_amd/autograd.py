@@ -1,7 +1,9 @@
-"""torch.autograd wrapper and nn.Module around the fused WTConv library.
+"""torch.autograd wrappers and nn.Modules around the fused WTConv library: the
+convolution, and the layer norm and scaled residual of the block around it.
 
-Only x and the parameters are saved for backward (no per-level subband
-tensors): the backward kernel recomputes both Haar pyramids on chip.
+Of the convolution, only x and the parameters are saved for backward (no
+per-level subband tensors): the backward kernel recomputes both Haar pyramids
+on chip. The layer norm saves x and two floats a pixel.
 """
 import ctypes
 import math
@@ -100,3 +102,91 @@ class WTConv2d(torch.nn.Module):
 
     def forward(self, x):
         return wtconv(x, self.base_w, self.base_scale, list(self.level_w), list(self.level_scale), self.base_bias)
+
+
+def _dense_rows(t):
+    return t if binding._row_stride(t) is not None else t.contiguous()
+
+
+class LayerNormFunction(torch.autograd.Function):
+    """layer_norm() of tensors as binding.norm_desc takes them."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, channel_dim, out_channel_dim):
+        y, mean, rstd = binding.layer_norm_forward(x, weight, bias, eps, channel_dim, out_channel_dim)
+        ctx.save_for_backward(x, mean, rstd, weight)
+        ctx.args = (eps, channel_dim, out_channel_dim)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, mean, rstd, weight = ctx.saved_tensors
+        dy = _dense_rows(dy) if ctx.args[2] == -1 else dy.contiguous()
+        grads = binding.layer_norm_backward(dy, x, mean, rstd, weight, *ctx.args, *ctx.needs_input_grad[:3])
+        return (*grads, None, None, None)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-6, channel_dim=-1, out_channel_dim=None):
+    """Layer norm over the channels of every pixel, under autograd:
+    (x - mean) / sqrt(variance + eps) * weight + bias.
+
+    The channels are dimension `channel_dim` of x, the last (-1: rows, x [..., C]) or dimension 1 (planes, x [B, C,
+    ...]), and dimension `out_channel_dim` of the result (by default the same one; 1 can be moved to -1, so that the
+    pointwise products that follow find the channels adjacent). x is float32, bfloat16 or float16, weight and bias
+    [C] float32 or None; sums are float32.
+    """
+    if out_channel_dim is None:
+        out_channel_dim = channel_dim
+    if channel_dim == 1 and isinstance(x, torch.Tensor) and x.dim() > 2 and not x.is_contiguous():
+        rows = x.movedim(1, -1)
+        if binding._row_stride(rows) is not None:  # planes held as rows (channels_last) are normalised as they lie
+            y = LayerNormFunction.apply(rows, weight, bias, eps, -1, -1)
+            return y if out_channel_dim == -1 else y.movedim(-1, 1)
+    if isinstance(x, torch.Tensor) and x.dim() > 1:
+        x = x.contiguous() if channel_dim == 1 else _dense_rows(x)
+    return LayerNormFunction.apply(x, weight, bias, eps, channel_dim, out_channel_dim)
+
+
+class ScaledResidualFunction(torch.autograd.Function):
+    """scaled_residual() of contiguous tensors."""
+
+    @staticmethod
+    def forward(ctx, x, z, gamma, sample_scale):
+        y = binding.scaled_residual_forward(x, z, gamma, sample_scale)
+        # z is needed for the gradient of gamma alone
+        ctx.save_for_backward(z if ctx.needs_input_grad[2] else None, gamma, sample_scale)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        z, gamma, sample_scale = ctx.saved_tensors
+        need_dx, need_dz, need_dgamma, _ = ctx.needs_input_grad
+        dy = dy.contiguous()
+        dz, dgamma = binding.scaled_residual_backward(dy, z, gamma, sample_scale, need_dz, need_dgamma)
+        return dy if need_dx else None, dz, dgamma, None
+
+
+def scaled_residual(x, z, gamma=None, sample_scale=None):
+    """x + sample_scale * gamma * z under autograd, where x [B, C, ...] and the result are planes and z [B, ..., C]
+    is rows, as the pointwise products leave them. gamma: [C] float32, the layer scale; sample_scale: [B] float32,
+    one factor an image (0 where stochastic depth drops the branch), a constant for autograd. None means ones."""
+    if isinstance(sample_scale, torch.Tensor) and sample_scale.requires_grad:
+        raise ValueError("sample_scale is a constant: it has no gradient")
+    if isinstance(x, torch.Tensor) and isinstance(z, torch.Tensor):
+        x, z = x.contiguous(), z.contiguous()
+    return ScaledResidualFunction.apply(x, z, gamma, sample_scale)
+
+
+class LayerNorm(torch.nn.Module):
+    """layer_norm() with its parameters, float32 whatever the activation dtype."""
+
+    def __init__(self, channels: int, eps: float = 1e-6, channel_dim: int = -1, out_channel_dim=None, device=None):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(channels, device=device))
+        self.bias = torch.nn.Parameter(torch.zeros(channels, device=device))
+        self.eps, self.channel_dim, self.out_channel_dim = eps, channel_dim, out_channel_dim
+
+    def forward(self, x):
+        return layer_norm(x, self.weight, self.bias, self.eps, self.channel_dim, self.out_channel_dim)

@@ -19,9 +19,16 @@ STATUS = {
 }
 EXPORTS = ["wtconv_forward_workspace_bytes", "wtconv_forward", "wtconv_backward", "wtconv_backward_workspace_bytes",
            "wtconv_backward_partials", "wtconv_backward_finalize", "wtconv_backward_data_workspace_bytes",
-           "wtconv_backward_data", "wtconv_backward_noalloc", "wtconv_status_string", "wtconv_version"]
+           "wtconv_backward_data", "wtconv_backward_noalloc", "wtconv_layer_norm_forward",
+           "wtconv_layer_norm_backward_workspace_bytes", "wtconv_layer_norm_backward",
+           "wtconv_scaled_residual_forward", "wtconv_scaled_residual_backward_workspace_bytes",
+           "wtconv_scaled_residual_backward", "wtconv_adamw_step", "wtconv_adamw_moments", "wtconv_status_string",
+           "wtconv_version"]
 NOALLOC_SCRATCH_BYTES = 64 << 20  # WTCONV_NOALLOC_SCRATCH_BYTES
 MAX_LEVELS = 8
+WTCONV_ROWS, WTCONV_PLANES = 0, 1
+MAX_CHANNELS = 1 << 20  # WTCONV_MAX_CHANNELS
+ADAMW_BLOCK = 64        # elements that share a scale of the 8-bit moments; offsets are multiples of it
 
 
 class WTConvError(RuntimeError):
@@ -33,6 +40,28 @@ class WTConvError(RuntimeError):
 class Desc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int), ("C", ctypes.c_int), ("H", ctypes.c_int), ("W", ctypes.c_int),
                 ("k", ctypes.c_int), ("L", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_longlong), ("S", ctypes.c_longlong), ("C", ctypes.c_int), ("in_", ctypes.c_int),
+                ("out", ctypes.c_int), ("x_stride", ctypes.c_longlong), ("dy_stride", ctypes.c_longlong),
+                ("eps", ctypes.c_double), ("dtype", ctypes.c_int)]
+
+
+class ResidualDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_longlong), ("S", ctypes.c_longlong), ("C", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class AdamWGroup(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", ctypes.c_longlong),
+                ("key", ctypes.c_uint), ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
+                ("exp_avg_scale", ctypes.c_void_p), ("exp_avg_sq_scale", ctypes.c_void_p)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("numel", ctypes.c_longlong),
+                ("offset", ctypes.c_longlong), ("group", ctypes.c_int)]
 
 
 _lib = None
@@ -71,6 +100,17 @@ def load():
     lib.wtconv_backward_noalloc.argtypes = [ctypes.POINTER(Desc), _P, _P, _P, _P, _P, _PP, _PP, _P, _P, _P, _P,
                                             _PP, _PP, _P]
     lib.wtconv_backward_noalloc.restype = ctypes.c_int
+    _N, _R, _Z = ctypes.POINTER(NormDesc), ctypes.POINTER(ResidualDesc), ctypes.c_size_t
+    lib.wtconv_layer_norm_forward.argtypes = [_N] + [_P] * 7
+    lib.wtconv_layer_norm_backward_workspace_bytes.argtypes = [_N]
+    lib.wtconv_layer_norm_backward_workspace_bytes.restype = _Z
+    lib.wtconv_layer_norm_backward.argtypes = [_N] + [_P] * 9 + [_Z, _P]
+    lib.wtconv_scaled_residual_forward.argtypes = [_R] + [_P] * 6
+    lib.wtconv_scaled_residual_backward_workspace_bytes.argtypes = [_R]
+    lib.wtconv_scaled_residual_backward_workspace_bytes.restype = _Z
+    lib.wtconv_scaled_residual_backward.argtypes = [_R] + [_P] * 7 + [_Z, _P]
+    lib.wtconv_adamw_step.argtypes = [ctypes.c_int, _P, ctypes.c_int, _P, ctypes.c_int, ctypes.c_int, _P, _P]
+    lib.wtconv_adamw_moments.argtypes = [ctypes.c_longlong, _P, _P, _P, _P, _P, _P, ctypes.c_int, _P]
     lib.wtconv_status_string.argtypes = [ctypes.c_int]
     lib.wtconv_status_string.restype = ctypes.c_char_p
     lib.wtconv_version.restype = ctypes.c_int
@@ -173,6 +213,45 @@ def wtconv_backward_data(desc: Desc, dy, base_w, base_scale, level_w, level_scal
     return load().wtconv_backward_data(ctypes.byref(desc), dy, base_w, base_scale, _ptr_array(level_w),
                                        _ptr_array(level_scale), dx, workspace, ctypes.c_size_t(workspace_bytes),
                                        stream)
+
+
+def wtconv_layer_norm_forward(desc: NormDesc, x, weight, bias, y, mean, rstd, stream) -> int:
+    return load().wtconv_layer_norm_forward(ctypes.byref(desc), x, weight, bias, y, mean, rstd, stream)
+
+
+def wtconv_layer_norm_backward_workspace_bytes(desc: NormDesc) -> int:
+    return int(load().wtconv_layer_norm_backward_workspace_bytes(ctypes.byref(desc)))
+
+
+def wtconv_layer_norm_backward(desc: NormDesc, dy, x, mean, rstd, weight, dx, d_weight, d_bias, workspace,
+                               workspace_bytes, stream) -> int:
+    return load().wtconv_layer_norm_backward(ctypes.byref(desc), dy, x, mean, rstd, weight, dx, d_weight, d_bias,
+                                             workspace, ctypes.c_size_t(workspace_bytes), stream)
+
+
+def wtconv_scaled_residual_forward(desc: ResidualDesc, x, z, gamma, sample_scale, y, stream) -> int:
+    return load().wtconv_scaled_residual_forward(ctypes.byref(desc), x, z, gamma, sample_scale, y, stream)
+
+
+def wtconv_scaled_residual_backward_workspace_bytes(desc: ResidualDesc) -> int:
+    return int(load().wtconv_scaled_residual_backward_workspace_bytes(ctypes.byref(desc)))
+
+
+def wtconv_scaled_residual_backward(desc: ResidualDesc, dy, z, gamma, sample_scale, dz, d_gamma, workspace,
+                                    workspace_bytes, stream) -> int:
+    return load().wtconv_scaled_residual_backward(ctypes.byref(desc), dy, z, gamma, sample_scale, dz, d_gamma,
+                                                  workspace, ctypes.c_size_t(workspace_bytes), stream)
+
+
+def wtconv_adamw_step(groups, tensors, dtype, state_bits, grad_scale, stream) -> int:
+    """groups, tensors: lists of AdamWGroup and AdamWTensor."""
+    return load().wtconv_adamw_step(len(groups), (AdamWGroup * max(1, len(groups)))(*groups), len(tensors),
+                                    (AdamWTensor * max(1, len(tensors)))(*tensors), dtype, state_bits, grad_scale,
+                                    stream)
+
+
+def wtconv_adamw_moments(n, exp_avg, exp_avg_scale, exp_avg_sq, exp_avg_sq_scale, m, v, dtype, stream) -> int:
+    return load().wtconv_adamw_moments(n, exp_avg, exp_avg_scale, exp_avg_sq, exp_avg_sq_scale, m, v, dtype, stream)
 
 
 def wtconv_version() -> int:
@@ -445,3 +524,191 @@ class Backward:
         _check(wtconv_backward_finalize(self.desc, bw.data_ptr(), bs.data_ptr(), None, self._lw, self._ls,
                                         self.dbw.data_ptr(), self.dbs.data_ptr(), None, self._dlw, self._dls,
                                         self.workspace.data_ptr(), self.nbytes, _stream(self.device)))
+
+
+# ----------------------------------------------------------------------------
+# the operators around the convolution in a network block
+# ----------------------------------------------------------------------------
+
+def _activation(t, name, on_gpu=True):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    if on_gpu and not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    if t.dim() < 2:
+        raise ValueError(f"{name} must have at least two dimensions, got shape {tuple(t.shape)}")
+
+
+def _row_stride(t):
+    """Elements from one row (the last dimension) to the next, or None where the rows do not lie at one distance
+    from each other or their elements are not adjacent."""
+    sizes, strides = t.shape, t.stride()
+    if sizes[-1] > 1 and strides[-1] != 1:
+        return None
+    stride = rows = None
+    for n, st in zip(reversed(sizes[:-1]), reversed(strides[:-1])):
+        if n == 1:
+            continue
+        if rows is None:
+            stride, rows = st, n
+        elif st != stride * rows:
+            return None
+        else:
+            rows *= n
+    if rows is None or t.numel() == 0:
+        return sizes[-1]
+    return stride if stride >= sizes[-1] else None
+
+
+def _dims(t, channel_dim):
+    """(B, S, C) of a tensor whose channels are the last dimension or dimension 1."""
+    n = t.numel()
+    C = t.shape[channel_dim]
+    if not 1 <= C <= MAX_CHANNELS:
+        raise ValueError(f"the channels must be 1 to {MAX_CHANNELS}, got {C}")
+    B = t.shape[0]
+    return B, n // (B * C) if n else 0, C
+
+
+def norm_desc(x, weight=None, bias=None, eps=1e-6, channel_dim=-1, out_channel_dim=None, dy=None, on_gpu=True):
+    """Check every tensor of a layer norm before anything reaches the library, and describe the problem: x [..., C]
+    (channel_dim = -1; rows at one distance from each other) or [B, C, ...] (channel_dim = 1; contiguous), weight
+    and bias [C] float32 or None; the output has its channels in out_channel_dim, -1 or 1, and can be moved from 1
+    to -1 but not back; dy as the output. Raises ValueError; returns (NormDesc, the output's shape)."""
+    import torch
+    _activation(x, "x", on_gpu)
+    out_channel_dim = channel_dim if out_channel_dim is None else out_channel_dim
+    if (channel_dim, out_channel_dim) not in ((-1, -1), (1, -1), (1, 1)):
+        raise ValueError(f"channels go from dimension -1 to -1, from 1 to -1 or from 1 to 1, not from {channel_dim} "
+                         f"to {out_channel_dim}")
+    B, S, C = _dims(x, channel_dim)
+    if not (isinstance(eps, (int, float)) and 0 <= eps < float("inf")):
+        raise ValueError(f"eps must be a number >= 0, got {eps}")
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            _require(t, name, torch.float32, (C,), x.device, on_gpu)
+    shape = tuple(x.shape)
+    if channel_dim == 1:
+        if not x.is_contiguous():
+            raise ValueError("x must be contiguous")
+        x_stride = 0
+        if out_channel_dim == -1:
+            shape = (shape[0], *shape[2:], C)
+    else:
+        x_stride = _row_stride(x)
+        if x_stride is None:
+            raise ValueError("the rows of x must be contiguous and at one distance from each other")
+    dy_stride = 0
+    if dy is not None:
+        _activation(dy, "dy", on_gpu)
+        if dy.dtype != x.dtype or dy.device != x.device or tuple(dy.shape) != shape:
+            raise ValueError(f"dy must be {x.dtype} of shape {shape} on {x.device}, got {dy.dtype} of shape "
+                             f"{tuple(dy.shape)} on {dy.device}")
+        if out_channel_dim == -1:
+            dy_stride = _row_stride(dy)
+        if dy_stride is None or (out_channel_dim == 1 and not dy.is_contiguous()):
+            raise ValueError("dy must be contiguous, or rows at one distance from each other")
+    desc = NormDesc(B, S, C, WTCONV_PLANES if channel_dim == 1 else WTCONV_ROWS,
+                    WTCONV_PLANES if out_channel_dim == 1 else WTCONV_ROWS, x_stride, dy_stride, float(eps),
+                    _dtype_code(x))
+    return desc, shape
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def layer_norm_forward(x, weight=None, bias=None, eps=1e-6, channel_dim=-1, out_channel_dim=None, stats=True):
+    """Layer norm over the channels on the current stream: (y, mean, rstd), the last two [pixels] float32 for the
+    backward pass, or None without stats. Tensors as norm_desc takes them."""
+    import torch
+    desc, shape = norm_desc(x, weight, bias, eps, channel_dim, out_channel_dim)
+    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    n = desc.B * desc.S
+    mean = torch.empty(n, dtype=torch.float32, device=x.device) if stats else None
+    rstd = torch.empty_like(mean) if stats else None
+    _check(wtconv_layer_norm_forward(desc, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean),
+                                     _ptr(rstd), _stream(x.device)))
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, eps=1e-6, channel_dim=-1, out_channel_dim=None, need_dx=True,
+                        need_dweight=True, need_dbias=True):
+    """Gradients of sum(y * dy): (dx, d_weight, d_bias), None for those not asked for; x, mean and rstd as
+    layer_norm_forward took and gave them."""
+    import torch
+    desc, _ = norm_desc(x, weight, None, eps, channel_dim, out_channel_dim, dy=dy)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _require(t, name, torch.float32, (desc.B * desc.S,), x.device)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_dx else None
+    dw = torch.empty(desc.C, dtype=torch.float32, device=x.device) if need_dweight else None
+    db = torch.empty(desc.C, dtype=torch.float32, device=x.device) if need_dbias else None
+    nbytes = wtconv_layer_norm_backward_workspace_bytes(desc) if need_dweight or need_dbias else 0
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
+    _check(wtconv_layer_norm_backward(desc, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                      _ptr(weight), _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws), nbytes,
+                                      _stream(x.device)))
+    return dx, dw, db
+
+
+def residual_desc(x, z, gamma=None, sample_scale=None, on_gpu=True):
+    """Check every tensor of a scaled residual: x [B, C, ...], z [B, ..., C], both contiguous and of one type, gamma
+    [C] and sample_scale [B] float32 or None. Raises ValueError; returns the ResidualDesc."""
+    import torch
+    _activation(x, "x", on_gpu)
+    B, S, C = _dims(x, 1)
+    _require(x, "x", on_gpu=on_gpu)
+    if z is not None:
+        _require(z, "z", x.dtype, (B, *x.shape[2:], C), x.device, on_gpu)
+    if gamma is not None:
+        _require(gamma, "gamma", torch.float32, (C,), x.device, on_gpu)
+    if sample_scale is not None:
+        _require(sample_scale, "sample_scale", torch.float32, (B,), x.device, on_gpu)
+    return ResidualDesc(B, S, C, _dtype_code(x))
+
+
+def scaled_residual_forward(x, z, gamma=None, sample_scale=None):
+    """y = x + sample_scale * gamma * z on the current stream, z's rows turned to planes."""
+    import torch
+    if z is None:
+        raise ValueError("z must be a tensor")
+    desc = residual_desc(x, z, gamma, sample_scale)
+    y = torch.empty_like(x)
+    _check(wtconv_scaled_residual_forward(desc, x.data_ptr(), z.data_ptr(), _ptr(gamma), _ptr(sample_scale),
+                                          y.data_ptr(), _stream(x.device)))
+    return y
+
+
+def scaled_residual_backward(dy, z, gamma=None, sample_scale=None, need_dz=True, need_dgamma=True):
+    """Gradients of sum(y * dy) with respect to z and gamma, None for those not asked for; that of x is dy. z may be
+    None where the gradient of gamma is not asked for."""
+    import torch
+    if z is None and need_dgamma:
+        raise ValueError("the gradient of gamma needs z")
+    desc = residual_desc(dy, z, gamma, sample_scale)
+    rows = (dy.shape[0], *dy.shape[2:], dy.shape[1])
+    dz = torch.empty(rows, dtype=dy.dtype, device=dy.device) if need_dz else None
+    dg = torch.empty(desc.C, dtype=torch.float32, device=dy.device) if need_dgamma else None
+    nbytes = wtconv_scaled_residual_backward_workspace_bytes(desc) if need_dgamma else 0
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dy.device) if nbytes else None
+    _check(wtconv_scaled_residual_backward(desc, dy.data_ptr(), _ptr(z), _ptr(gamma), _ptr(sample_scale),
+                                           _ptr(dz), _ptr(dg), _ptr(ws), nbytes, _stream(dy.device)))
+    return dz, dg
+
+
+def adamw_moments(exp_avg, exp_avg_scale, exp_avg_sq, exp_avg_sq_scale, dtype):
+    """The values that whole buffers of 8-bit moments stand for: (m, v) of `dtype`."""
+    import torch
+    n = exp_avg.numel()
+    for name, t, size in (("exp_avg", exp_avg, n), ("exp_avg_scale", exp_avg_scale, n // ADAMW_BLOCK),
+                          ("exp_avg_sq", exp_avg_sq, n), ("exp_avg_sq_scale", exp_avg_sq_scale, n // ADAMW_BLOCK)):
+        _require(t, name, torch.uint8, (size,), exp_avg.device)
+    m = torch.empty(n, dtype=dtype, device=exp_avg.device)
+    v = torch.empty_like(m)
+    _check(wtconv_adamw_moments(n, exp_avg.data_ptr(), exp_avg_scale.data_ptr(), exp_avg_sq.data_ptr(),
+                                exp_avg_sq_scale.data_ptr(), m.data_ptr(), v.data_ptr(), _dtype_code(m),
+                                _stream(m.device)))
+    return m, v

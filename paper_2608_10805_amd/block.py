@@ -1,0 +1,111 @@
+"""A network block around the wavelet convolution, in the order ConvNeXt has it:
+convolution -> layer norm over the channels -> pointwise products with a GELU
+between -> layer scale, stochastic depth and residual. The convolution works on
+planes, the products on rows of channels; the norm and the residual change from
+one to the other, so no pass only moves data.
+
+Run as a program it trains a small network of such blocks on synthetic images:
+
+    python -m paper_2608_10805_amd.block [--steps N] [--state-bits 8|32] [--dtype f32|bf16|f16]
+"""
+import torch
+import torch.nn.functional as F
+
+from .autograd import LayerNorm, WTConv2d, scaled_residual
+
+
+class WTConvNeXtBlock(torch.nn.Module):
+    """x [B, C, H, W] -> the same shape and type. The convolution's, norm's and layer scale's parameters are float32;
+    the products run in x's type. `drop_path` is the probability that training drops an image's branch."""
+
+    def __init__(self, channels, kernel_size=5, levels=3, hidden=None, layer_scale=1e-6, drop_path=0.0, device=None):
+        super().__init__()
+        if not 0 <= drop_path < 1:
+            raise ValueError(f"drop_path must be in [0, 1), got {drop_path}")
+        hidden = 4 * channels if hidden is None else hidden
+        self.conv = WTConv2d(channels, kernel_size, levels, bias=True, device=device)
+        self.norm = LayerNorm(channels, channel_dim=1, out_channel_dim=-1, device=device)
+        self.expand = torch.nn.Linear(channels, hidden, device=device)
+        self.project = torch.nn.Linear(hidden, channels, device=device)
+        self.gamma = torch.nn.Parameter(torch.full((channels,), layer_scale, device=device))
+        self.drop_path = drop_path
+
+    def forward(self, x):
+        z = self.norm(self.conv(x))
+        for i, product in enumerate((self.expand, self.project)):
+            z = F.linear(z, product.weight.to(x.dtype), product.bias.to(x.dtype))
+            if i == 0:
+                z = F.gelu(z)
+        keep = None
+        if self.training and self.drop_path:
+            keep = (torch.rand(x.shape[0], device=x.device) >= self.drop_path).float() / (1 - self.drop_path)
+        return scaled_residual(x, z, self.gamma, keep)
+
+
+class WTConvNeXt(torch.nn.Module):
+    """Patches of 4 x 4 pixels, stages of blocks with a norm and a 2 x 2 convolution between, a classifier."""
+
+    def __init__(self, widths=(16, 32), depths=(2, 2), classes=10, kernel_size=5, levels=2, layer_scale=1e-2,
+                 drop_path=0.0, device=None):
+        super().__init__()
+        conv = lambda i, o, k: torch.nn.Conv2d(i, o, k, stride=k, device=device)  # noqa: E731
+        layers = [conv(3, widths[0], 4), LayerNorm(widths[0], channel_dim=1, device=device)]
+        for i, (C, depth) in enumerate(zip(widths, depths)):
+            if i:
+                layers += [LayerNorm(widths[i - 1], channel_dim=1, device=device), conv(widths[i - 1], C, 2)]
+            layers += [WTConvNeXtBlock(C, kernel_size, levels, layer_scale=layer_scale, drop_path=drop_path,
+                                       device=device) for _ in range(depth)]
+        self.layers = torch.nn.ModuleList(layers)
+        self.norm = LayerNorm(widths[-1], device=device)
+        self.head = torch.nn.Linear(widths[-1], classes, device=device)
+
+    def forward(self, x):
+        for layer in self.layers:
+            if isinstance(layer, torch.nn.Conv2d):
+                x = F.conv2d(x, layer.weight.to(x.dtype), layer.bias.to(x.dtype), layer.stride)
+            else:
+                x = layer(x)
+        x = self.norm(x.mean((2, 3)))
+        return F.linear(x, self.head.weight.to(x.dtype), self.head.bias.to(x.dtype)).float()
+
+
+def decay_groups(model, weight_decay):
+    """Parameter groups as such networks are trained: matrices and kernels decay, vectors do not."""
+    split = [[p for p in model.parameters() if (p.dim() > 1) == decayed] for decayed in (True, False)]
+    return [{"params": split[0], "weight_decay": weight_decay}, {"params": split[1], "weight_decay": 0.0}]
+
+
+def train(steps=30, state_bits=32, dtype=torch.float32, seed=0, device="cuda", batch=32, size=64, log=None):
+    """Train the small network to tell which of ten gratings a noisy image shows; returns the losses."""
+    from .optim import AdamW
+
+    torch.manual_seed(seed)
+    model = WTConvNeXt(drop_path=0.05, device=device)
+    opt = AdamW(decay_groups(model, 0.05), lr=2e-3, state_bits=state_bits, seed=seed)
+    at = torch.arange(size, device=device, dtype=torch.float32)
+    losses = []
+    for step in range(steps):
+        label = torch.randint(10, (batch,), device=device)
+        angle = label.view(-1, 1, 1) * (torch.pi / 10)
+        wave = torch.sin((at.view(1, -1, 1) * angle.sin() + at.view(1, 1, -1) * angle.cos()) * 0.7)
+        images = (wave.unsqueeze(1) + 0.3 * torch.randn(batch, 3, size, size, device=device)).to(dtype)
+        opt.zero_grad()
+        loss = F.cross_entropy(model(images), label)
+        loss.backward()
+        opt.step()
+        losses.append(loss.detach())
+        if log and (step % 10 == 9 or step == 0):
+            log(f"step {step + 1}: loss {losses[-1].item():.3f}")
+    return torch.stack(losses).tolist()
+
+
+if __name__ == "__main__":
+    import argparse
+
+    ap = argparse.ArgumentParser(description="Train a small wavelet-convolution network on synthetic images.")
+    ap.add_argument("--steps", type=int, default=100)
+    ap.add_argument("--state-bits", type=int, choices=(8, 32), default=32)
+    ap.add_argument("--dtype", choices=("f32", "bf16", "f16"), default="f32")
+    args = ap.parse_args()
+    train(args.steps, args.state_bits, {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[args.dtype],
+          log=lambda line: print(line, flush=True))

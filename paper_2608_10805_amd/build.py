@@ -14,11 +14,13 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
+CSRC_BLOCK = os.path.join(HERE, "csrc_block")  # the operators around the convolution
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libwtconv.so")
 SOURCES = ["wtconv_api.cpp", "wtconv_noalloc.cpp", "wtconv_fwd.hip", "wtconv_mixed.hip", "wtconv_bwd.hip",
            "wtconv_bwd9.hip", "wtconv_phase_fwd.hip", "wtconv_phase_grad.hip", "wtconv_grad.hip",
            "wtconv_kernels.hip", "wtconv_tiny.hip"]
+BLOCK_SOURCES = ["block_api.cpp", "norm.hip", "residual.hip", "adamw.hip"]
 # measurement helper used only by the benchmark (sustained VALU rate)
 PROBE_LIB = os.path.join(HERE, "libvalu_probe.so")
 PROBE_SOURCES = ["valu_probe.hip"]
@@ -35,14 +37,15 @@ def hipcc():
 def hipcc_flags():
     return ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall",
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-            "-I", INCLUDE, "-I", CSRC]
+            "-I", INCLUDE, "-I", CSRC, "-I", CSRC_BLOCK]
 
 
 def _compile(sources, lib, extra, verbose):
     with tempfile.TemporaryDirectory(prefix="wtconv_build_") as tmp:
         def one(src):
             obj = os.path.join(tmp, src + ".o")
-            cmd = [hipcc()] + hipcc_flags() + list(extra or []) + ["-x", "hip", "-c", os.path.join(CSRC, src),
+            folder = CSRC_BLOCK if src in BLOCK_SOURCES else CSRC
+            cmd = [hipcc()] + hipcc_flags() + list(extra or []) + ["-x", "hip", "-c", os.path.join(folder, src),
                                                                     "-o", obj]
             if verbose:
                 print(" ".join(cmd), flush=True)
@@ -102,7 +105,7 @@ def build(verbose: bool = False, extra=None) -> str:
     """Compile every HIP source (libwtconv.so and the benchmark's VALU probe) and
     the autograd wrapper's native host path (where g++ and torch's headers are
     there); return the path of libwtconv.so."""
-    _compile(SOURCES, LIB, extra, verbose)
+    _compile(SOURCES + BLOCK_SOURCES, LIB, extra, verbose)
     _compile_torch(verbose)
     _compile(PROBE_SOURCES, PROBE_LIB, extra, verbose)
     return LIB

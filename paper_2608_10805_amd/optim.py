@@ -1,0 +1,209 @@
+"""AdamW over every tensor of a network at once, with moments in 32 or in 8 bits.
+
+A network of wavelet convolutions has many small tensors (a kernel and a scale
+for each level and layer). One step takes one launch for every 88 of them; the
+moments of a parameter group lie in two buffers, one after the other.
+"""
+import torch
+
+from . import binding
+
+_M32 = 0xFFFFFFFF
+_DTYPES = (torch.float32, torch.bfloat16, torch.float16)
+
+
+def _mix(x):
+    x = ((x ^ (x >> 15)) * 0x85EBCA6B) & _M32
+    x = ((x ^ (x >> 13)) * 0xC2B2AE35) & _M32
+    return x ^ (x >> 16)
+
+
+def rounding_key(seed, step, group):
+    """The key of the random bits that round one group's 8-bit moments in one step."""
+    a = _mix((seed * 0x9E3779B1 + step * 0x9E3779B9) & _M32)
+    return _mix((group * 0x9E3779B1 + a) & _M32)
+
+
+def _strides_fill(t):
+    """Whether the tensor's elements fill one run of memory, in any order of its dimensions."""
+    return t.is_contiguous() or (t.dim() == 4 and t.is_contiguous(memory_format=torch.channels_last)) or \
+        (t.dim() == 5 and t.is_contiguous(memory_format=torch.channels_last_3d))
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW (decoupled weight decay) on GPU parameters in float32, bfloat16 or float16:
+
+        m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+        p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+
+    computed in float32 and rounded to the parameter's type once. With `state_bits` = 32 the moments are float32. With
+    8 they take one byte an element and one for every 64 elements, as small floats under a shared power of two; they
+    are rounded at random, by bits that depend on `seed`, the step and the element alone, so that a step that is
+    repeated gives the same bits. A block of 64 that meets a value that is not finite stands for NaN from then on, as
+    a 32-bit moment does.
+
+    The moments are allocated with the group. `state[p]` holds views of them: "exp_avg" and "exp_avg_sq" (shaped as p
+    with 32 bits; the codes, one a element in the order of memory, with 8), "exp_avg_scale" and "exp_avg_sq_scale" (8
+    bits), and "step", the number of steps p has taken. A parameter without a gradient is left alone.
+    """
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, seed=0):
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits must be 8 or 32, got {state_bits}")
+        self.state_bits, self.seed = state_bits, int(seed)
+        self._buffers = []  # of each group: exp_avg, exp_avg_sq, their scales (8 bits), steps, offsets
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        group = self.param_groups[-1]
+        try:
+            self._check_group(group)
+            self._allocate(group)
+        except ValueError:
+            self.param_groups.pop()
+            raise
+
+    def _check_group(self, group):
+        _hyperparameters(group)
+        devices = {p.device for g in self.param_groups for p in g["params"]}
+        for p in group["params"]:
+            if not p.is_cuda:
+                raise ValueError("AdamW steps GPU tensors only")
+            if p.dtype not in _DTYPES:
+                raise ValueError(f"parameters must be float32, bfloat16 or float16, got {p.dtype}")
+            if p.layout != torch.strided or not _strides_fill(p):
+                raise ValueError(f"a parameter of shape {tuple(p.shape)} and strides {p.stride()} does not fill its "
+                                 "memory")
+        if len(devices) > 1:
+            raise ValueError(f"all parameters must be on one device, got {sorted(map(str, devices))}")
+
+    def _allocate(self, group):
+        block, params, offsets, end = binding.ADAMW_BLOCK, group["params"], [], 0
+        for p in params:
+            offsets.append(end)
+            end += -(-p.numel() // block) * block
+        coded = self.state_bits == 8
+        new = lambda n: torch.zeros(n, dtype=torch.uint8 if coded else torch.float32,  # noqa: E731
+                                    device=params[0].device if params else "cpu")
+        buffers = {"exp_avg": new(end), "exp_avg_sq": new(end)}
+        if coded:
+            buffers.update(exp_avg_scale=new(end // block), exp_avg_sq_scale=new(end // block))
+        buffers.update(step=torch.zeros(len(params), dtype=torch.int64), offsets=offsets,
+                       numel=[p.numel() for p in params])
+        self._buffers.append(buffers)
+        for i, (p, at) in enumerate(zip(params, offsets)):
+            n, state = p.numel(), {"step": buffers["step"][i]}
+            for name in ("exp_avg", "exp_avg_sq"):
+                if coded:
+                    state[name] = buffers[name][at:at + n]
+                    state[name + "_scale"] = buffers[name + "_scale"][at // block:at // block - (-n // block)]
+                else:
+                    state[name] = buffers[name][at:at + n].as_strided(p.shape, p.stride())
+            self.state[p] = state
+
+    @torch.no_grad()
+    def step(self, closure=None, grad_scale=None):
+        """One step. grad_scale: a float32 GPU tensor of one element that every gradient is multiplied with (to undo
+        a loss scale, or to clip), or None."""
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("an AdamW step cannot be captured: the bias corrections of its step would be replayed")
+        self._step(grad_scale)
+        return loss
+
+    def _step(self, grad_scale):
+        device, taken, calls = None, [], {}  # calls: by the parameters' type, (groups, tensors)
+        for index, (group, buffers) in enumerate(zip(self.param_groups, self._buffers)):
+            lr, beta1, beta2, eps, decay = _hyperparameters(group)
+            places = {}  # of (type, step) in the call's groups
+            steps = buffers["step"].tolist()
+            for i, p in enumerate(group["params"]):
+                if p.grad is None:
+                    continue
+                grad = _gradient(p, buffers, i)
+                device, step = p.device, steps[i] + 1
+                code = binding._dtype_code(p)
+                groups, tensors = calls.setdefault(code, ([], []))
+                if (code, step) not in places:
+                    places[code, step] = len(groups)
+                    scales = [buffers[n].data_ptr() if n in buffers else None
+                              for n in ("exp_avg_scale", "exp_avg_sq_scale")]
+                    groups.append(binding.AdamWGroup(lr, beta1, beta2, eps, decay, step,
+                                                     rounding_key(self.seed, step, index),
+                                                     buffers["exp_avg"].data_ptr(), buffers["exp_avg_sq"].data_ptr(),
+                                                     *scales))
+                tensors.append(binding.AdamWTensor(p.data_ptr(), grad.data_ptr(), p.numel(), buffers["offsets"][i],
+                                                   places[code, step]))
+                taken.append((buffers["step"], i, p, grad))  # a gradient that was copied lives until the launch
+        if device is None:
+            return
+        if grad_scale is not None:
+            binding._require(grad_scale, "grad_scale", torch.float32, device=device)
+            if grad_scale.numel() != 1:
+                raise ValueError(f"grad_scale must have one element, got shape {tuple(grad_scale.shape)}")
+        stream = binding._stream(device)
+        for code, (groups, tensors) in calls.items():
+            binding._check(binding.wtconv_adamw_step(groups, tensors, code, self.state_bits,
+                                                     binding._ptr(grad_scale), stream))
+        for steps, i, _, _ in taken:
+            steps[i] += 1
+        torch.autograd.graph.increment_version([p for _, _, p, _ in taken])
+
+    def moments(self, dtype=torch.bfloat16):
+        """(exp_avg, exp_avg_sq) of each group, every parameter's from its first element's place on (a multiple of
+        64). With 32 bits these are the buffers themselves; with 8 bits the values that the codes stand for, as new
+        tensors of `dtype` (bfloat16 holds each exactly down to 2^-126)."""
+        if self.state_bits == 32:
+            return [(b["exp_avg"], b["exp_avg_sq"]) for b in self._buffers]
+        return [binding.adamw_moments(b["exp_avg"], b["exp_avg_scale"], b["exp_avg_sq"], b["exp_avg_sq_scale"], dtype)
+                for b in self._buffers]
+
+    def load_state_dict(self, state_dict):
+        """Copy the hyperparameters and the moments of a state_dict() of an optimizer with the same groups, shapes and
+        state_bits into this one."""
+        saved, groups = state_dict["state"], state_dict["param_groups"]
+        if [len(g["params"]) for g in groups] != [len(g["params"]) for g in self.param_groups]:
+            raise ValueError("the state has other parameter groups")
+        pairs = [(p, saved[i]) for ours, g in zip(self.param_groups, groups) for p, i in zip(ours["params"], g["params"])
+                 if i in saved]
+        for p, state in pairs:
+            ours = self.state[p]
+            if set(state) != set(ours) or any(state[k].shape != ours[k].shape or state[k].dtype != ours[k].dtype
+                                              for k in ours):
+                raise ValueError("the state is not of these parameters, or was held in other bits")
+        for p, state in pairs:
+            for k, t in self.state[p].items():
+                t.copy_(state[k])
+        for ours, g in zip(self.param_groups, groups):
+            ours.update({k: v for k, v in g.items() if k != "params"})
+
+
+def _gradient(p, buffers, i):
+    """The gradient of the group's parameter i, in the order of its memory."""
+    grad = p.grad
+    if grad.layout != torch.strided:
+        raise ValueError("AdamW takes dense gradients only")
+    if p.numel() != buffers["numel"][i] or p.dtype not in _DTYPES or p.device != buffers["exp_avg"].device or \
+            not _strides_fill(p):
+        raise ValueError(f"a parameter of shape {tuple(p.shape)} changed its size, type, device or order of memory")
+    if grad.dtype != p.dtype or grad.device != p.device:
+        raise ValueError(f"a gradient is {grad.dtype} on {grad.device}, its parameter {p.dtype} on {p.device}")
+    if grad.stride() != p.stride() or not _strides_fill(grad):
+        grad = torch.empty_like(p, requires_grad=False).copy_(grad)
+    return grad
+
+
+def _hyperparameters(group):
+    """(lr, beta1, beta2, eps, weight_decay) of a group as numbers, checked."""
+    lr, (beta1, beta2), eps, decay = float(group["lr"]), group["betas"], group["eps"], group["weight_decay"]
+    for name, v in (("lr", lr), ("eps", eps), ("weight_decay", decay)):
+        if not 0 <= v < float("inf"):
+            raise ValueError(f"{name} must be a number >= 0, got {v}")
+    for v in (beta1, beta2):
+        if not 0 <= v < 1:
+            raise ValueError(f"betas must be in [0, 1), got {group['betas']}")
+    return lr, float(beta1), float(beta2), float(eps), float(decay)
