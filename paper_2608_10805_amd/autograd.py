@@ -104,6 +104,31 @@ class WTConv2d(torch.nn.Module):
         return wtconv(x, self.base_w, self.base_scale, list(self.level_w), list(self.level_scale), self.base_bias)
 
 
+_block = None
+
+
+def load_block(x):
+    """The native host path of the operators around the convolution (csrc_block/block_torch.cpp), given the library's
+    entry points; False where it was not built, and for an x that is no GPU tensor (nothing is loaded for it)."""
+    global _block
+    if not (isinstance(x, torch.Tensor) and x.is_cuda):
+        return False
+    if _block is None:
+        try:
+            from . import _wtconv_block as ext
+        except ImportError:
+            _block = False
+        else:
+            lib = binding.load()
+            ext.init([ctypes.cast(getattr(lib, n), ctypes.c_void_p).value
+                      for n in ("wtconv_layer_norm_forward", "wtconv_layer_norm_backward_workspace_bytes",
+                                "wtconv_layer_norm_backward", "wtconv_scaled_residual_forward",
+                                "wtconv_scaled_residual_backward_workspace_bytes", "wtconv_scaled_residual_backward",
+                                "wtconv_adamw_step")], _norm_backward, _residual_backward)
+            _block = ext
+    return _block
+
+
 def _dense_rows(t):
     return t if binding._row_stride(t) is not None else t.contiguous()
 
@@ -119,12 +144,15 @@ class LayerNormFunction(torch.autograd.Function):
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        x, mean, rstd, weight = ctx.saved_tensors
-        dy = _dense_rows(dy) if ctx.args[2] == -1 else dy.contiguous()
-        grads = binding.layer_norm_backward(dy, x, mean, rstd, weight, *ctx.args, *ctx.needs_input_grad[:3])
-        return (*grads, None, None, None)
+        return (*_norm_backward((*ctx.args, *ctx.needs_input_grad[:3]), dy, *ctx.saved_tensors), None, None, None)
+
+
+@torch.autograd.function.once_differentiable
+def _norm_backward(args, dy, x, mean, rstd, weight):
+    """args: eps, the two channel dimensions and which gradients are asked for."""
+    dy = _dense_rows(dy) if args[2] == -1 else dy.contiguous()
+    return binding.layer_norm_backward(dy, x, mean, rstd, weight, *args)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-6, channel_dim=-1, out_channel_dim=None):
@@ -138,10 +166,15 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, channel_dim=-1, out_channel_
     """
     if out_channel_dim is None:
         out_channel_dim = channel_dim
+    ext = _block if _block is not None else load_block(x)
+    if ext and not torch.compiler.is_compiling():
+        y = ext.layer_norm(x, weight, bias, eps, channel_dim, out_channel_dim)
+        if y is not None:
+            return y
     if channel_dim == 1 and isinstance(x, torch.Tensor) and x.dim() > 2 and not x.is_contiguous():
         rows = x.movedim(1, -1)
         if binding._row_stride(rows) is not None:  # planes held as rows (channels_last) are normalised as they lie
-            y = LayerNormFunction.apply(rows, weight, bias, eps, -1, -1)
+            y = layer_norm(rows, weight, bias, eps)
             return y if out_channel_dim == -1 else y.movedim(-1, 1)
     if isinstance(x, torch.Tensor) and x.dim() > 1:
         x = x.contiguous() if channel_dim == 1 else _dense_rows(x)
@@ -159,19 +192,27 @@ class ScaledResidualFunction(torch.autograd.Function):
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        z, gamma, sample_scale = ctx.saved_tensors
-        need_dx, need_dz, need_dgamma, _ = ctx.needs_input_grad
-        dy = dy.contiguous()
-        dz, dgamma = binding.scaled_residual_backward(dy, z, gamma, sample_scale, need_dz, need_dgamma)
-        return dy if need_dx else None, dz, dgamma, None
+        return (*_residual_backward(ctx.needs_input_grad[:3], dy, *ctx.saved_tensors), None)
+
+
+@torch.autograd.function.once_differentiable
+def _residual_backward(need, dy, z, gamma, sample_scale):
+    """need: which of the gradients of x, z and gamma are asked for."""
+    dy = dy.contiguous()
+    dz, dgamma = binding.scaled_residual_backward(dy, z, gamma, sample_scale, *need[1:])
+    return dy if need[0] else None, dz, dgamma
 
 
 def scaled_residual(x, z, gamma=None, sample_scale=None):
     """x + sample_scale * gamma * z under autograd, where x [B, C, ...] and the result are planes and z [B, ..., C]
     is rows, as the pointwise products leave them. gamma: [C] float32, the layer scale; sample_scale: [B] float32,
     one factor an image (0 where stochastic depth drops the branch), a constant for autograd. None means ones."""
+    ext = _block if _block is not None else load_block(x)
+    if ext and not torch.compiler.is_compiling():
+        y = ext.scaled_residual(x, z, gamma, sample_scale)
+        if y is not None:
+            return y
     if isinstance(sample_scale, torch.Tensor) and sample_scale.requires_grad:
         raise ValueError("sample_scale is a constant: it has no gradient")
     if isinstance(x, torch.Tensor) and isinstance(z, torch.Tensor):

@@ -621,17 +621,24 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
+def _on(device):
+    """Kernels are launched with the tensors' device current."""
+    import torch
+    return torch.cuda.device(device)
+
+
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-6, channel_dim=-1, out_channel_dim=None, stats=True):
     """Layer norm over the channels on the current stream: (y, mean, rstd), the last two [pixels] float32 for the
     backward pass, or None without stats. Tensors as norm_desc takes them."""
     import torch
     desc, shape = norm_desc(x, weight, bias, eps, channel_dim, out_channel_dim)
-    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    y = x.new_empty(shape)
     n = desc.B * desc.S
     mean = torch.empty(n, dtype=torch.float32, device=x.device) if stats else None
     rstd = torch.empty_like(mean) if stats else None
-    _check(wtconv_layer_norm_forward(desc, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean),
-                                     _ptr(rstd), _stream(x.device)))
+    with _on(x.device):
+        _check(wtconv_layer_norm_forward(desc, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean),
+                                         _ptr(rstd), _stream(x.device)))
     return y, mean, rstd
 
 
@@ -643,14 +650,15 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, eps=1e-6, channel_dim=-1
     desc, _ = norm_desc(x, weight, None, eps, channel_dim, out_channel_dim, dy=dy)
     for name, t in (("mean", mean), ("rstd", rstd)):
         _require(t, name, torch.float32, (desc.B * desc.S,), x.device)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_dx else None
+    dx = x.new_empty(x.shape) if need_dx else None
     dw = torch.empty(desc.C, dtype=torch.float32, device=x.device) if need_dweight else None
     db = torch.empty(desc.C, dtype=torch.float32, device=x.device) if need_dbias else None
     nbytes = wtconv_layer_norm_backward_workspace_bytes(desc) if need_dweight or need_dbias else 0
     ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
-    _check(wtconv_layer_norm_backward(desc, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                      _ptr(weight), _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws), nbytes,
-                                      _stream(x.device)))
+    with _on(x.device):
+        _check(wtconv_layer_norm_backward(desc, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                          _ptr(weight), _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws), nbytes,
+                                          _stream(x.device)))
     return dx, dw, db
 
 
@@ -677,8 +685,9 @@ def scaled_residual_forward(x, z, gamma=None, sample_scale=None):
         raise ValueError("z must be a tensor")
     desc = residual_desc(x, z, gamma, sample_scale)
     y = torch.empty_like(x)
-    _check(wtconv_scaled_residual_forward(desc, x.data_ptr(), z.data_ptr(), _ptr(gamma), _ptr(sample_scale),
-                                          y.data_ptr(), _stream(x.device)))
+    with _on(x.device):
+        _check(wtconv_scaled_residual_forward(desc, x.data_ptr(), z.data_ptr(), _ptr(gamma), _ptr(sample_scale),
+                                              y.data_ptr(), _stream(x.device)))
     return y
 
 
@@ -690,12 +699,13 @@ def scaled_residual_backward(dy, z, gamma=None, sample_scale=None, need_dz=True,
         raise ValueError("the gradient of gamma needs z")
     desc = residual_desc(dy, z, gamma, sample_scale)
     rows = (dy.shape[0], *dy.shape[2:], dy.shape[1])
-    dz = torch.empty(rows, dtype=dy.dtype, device=dy.device) if need_dz else None
+    dz = dy.new_empty(rows) if need_dz else None
     dg = torch.empty(desc.C, dtype=torch.float32, device=dy.device) if need_dgamma else None
     nbytes = wtconv_scaled_residual_backward_workspace_bytes(desc) if need_dgamma else 0
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dy.device) if nbytes else None
-    _check(wtconv_scaled_residual_backward(desc, dy.data_ptr(), _ptr(z), _ptr(gamma), _ptr(sample_scale),
-                                           _ptr(dz), _ptr(dg), _ptr(ws), nbytes, _stream(dy.device)))
+    with _on(dy.device):
+        _check(wtconv_scaled_residual_backward(desc, dy.data_ptr(), _ptr(z), _ptr(gamma), _ptr(sample_scale),
+                                               _ptr(dz), _ptr(dg), _ptr(ws), nbytes, _stream(dy.device)))
     return dz, dg
 
 
@@ -708,7 +718,8 @@ def adamw_moments(exp_avg, exp_avg_scale, exp_avg_sq, exp_avg_sq_scale, dtype):
         _require(t, name, torch.uint8, (size,), exp_avg.device)
     m = torch.empty(n, dtype=dtype, device=exp_avg.device)
     v = torch.empty_like(m)
-    _check(wtconv_adamw_moments(n, exp_avg.data_ptr(), exp_avg_scale.data_ptr(), exp_avg_sq.data_ptr(),
-                                exp_avg_sq_scale.data_ptr(), m.data_ptr(), v.data_ptr(), _dtype_code(m),
-                                _stream(m.device)))
+    with _on(exp_avg.device):
+        _check(wtconv_adamw_moments(n, exp_avg.data_ptr(), exp_avg_scale.data_ptr(), exp_avg_sq.data_ptr(),
+                                    exp_avg_sq_scale.data_ptr(), m.data_ptr(), v.data_ptr(), _dtype_code(m),
+                                    _stream(m.device)))
     return m, v

@@ -27,6 +27,8 @@ PROBE_SOURCES = ["valu_probe.hip"]
 # native host path of the autograd wrapper: a Python extension against torch's headers
 TORCH_LIB = os.path.join(HERE, "_wtconv_torch.so")
 TORCH_SOURCE = "wtconv_torch.cpp"
+# the same for the operators around the convolution, next to it
+BLOCK_TORCH_NAME, BLOCK_TORCH_SOURCE = "_wtconv_block", "block_torch.cpp"
 ARCH = os.environ.get("WTCONV_OFFLOAD_ARCH", "gfx950")
 
 
@@ -78,33 +80,42 @@ def _torch_toolchain():
 def _compile_torch(verbose):
     import sysconfig
 
+    modules = [(os.path.join(CSRC, TORCH_SOURCE), TORCH_LIB),
+               (os.path.join(CSRC_BLOCK, BLOCK_TORCH_SOURCE),
+                os.path.join(os.path.dirname(TORCH_LIB), BLOCK_TORCH_NAME + ".so"))]
     found = _torch_toolchain()
     if found is None:
         print("no g++ or no torch headers: the autograd wrapper's native host path is left out", flush=True)
-        if os.path.exists(TORCH_LIB):  # (of other sources, perhaps)
-            os.remove(TORCH_LIB)
+        for _, lib in modules:
+            if os.path.exists(lib):  # (of other sources, perhaps)
+                os.remove(lib)
         return
     import torch
     gxx, t = found
     includes = [os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
                 os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"), sysconfig.get_paths()["include"]]
-    cmd = [gxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-           "-DTORCH_EXTENSION_NAME=_wtconv_torch",
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I", INCLUDE]
-    for d in includes:
-        cmd += ["-isystem", d]
-    cmd += [os.path.join(CSRC, TORCH_SOURCE), "-o", TORCH_LIB + ".tmp", "-L", os.path.join(t, "lib"), "-lc10",
-            "-lc10_hip", "-ltorch_cpu", "-ltorch", "-ltorch_python"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
-    os.replace(TORCH_LIB + ".tmp", TORCH_LIB)
+
+    def one(source, lib, name):
+        cmd = [gxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+               "-DTORCH_EXTENSION_NAME=" + name,
+               "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I", INCLUDE]
+        for d in includes:
+            cmd += ["-isystem", d]
+        cmd += [source, "-o", lib + ".tmp", "-L", os.path.join(t, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu",
+                "-ltorch", "-ltorch_python"]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+        os.replace(lib + ".tmp", lib)
+
+    with ThreadPoolExecutor(max_workers=len(modules)) as pool:
+        list(pool.map(lambda m: one(*m, os.path.basename(m[1])[:-len(".so")]), modules))
 
 
 def build(verbose: bool = False, extra=None) -> str:
     """Compile every HIP source (libwtconv.so and the benchmark's VALU probe) and
-    the autograd wrapper's native host path (where g++ and torch's headers are
-    there); return the path of libwtconv.so."""
+    the native host paths of the Python wrappers (where g++ and torch's headers
+    are there); return the path of libwtconv.so."""
     _compile(SOURCES + BLOCK_SOURCES, LIB, extra, verbose)
     _compile_torch(verbose)
     _compile(PROBE_SOURCES, PROBE_LIB, extra, verbose)

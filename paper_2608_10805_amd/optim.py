@@ -6,7 +6,7 @@ moments of a parameter group lie in two buffers, one after the other.
 """
 import torch
 
-from . import binding
+from . import autograd, binding
 
 _M32 = 0xFFFFFFFF
 _DTYPES = (torch.float32, torch.bfloat16, torch.float16)
@@ -51,7 +51,8 @@ class AdamW(torch.optim.Optimizer):
         if state_bits not in (8, 32):
             raise ValueError(f"state_bits must be 8 or 32, got {state_bits}")
         self.state_bits, self.seed = state_bits, int(seed)
-        self._buffers = []  # of each group: exp_avg, exp_avg_sq, their scales (8 bits), steps, offsets
+        self._buffers = []  # of each group: exp_avg, exp_avg_sq, their scales (8 bits), step, offsets, numel
+        self._native = []   # the same for the native host path
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
 
     def add_param_group(self, param_group):
@@ -92,6 +93,10 @@ class AdamW(torch.optim.Optimizer):
         buffers.update(step=torch.zeros(len(params), dtype=torch.int64), offsets=offsets,
                        numel=[p.numel() for p in params])
         self._buffers.append(buffers)
+        ext = autograd.load_block(params[0]) if params else False
+        self._native.append(ext.AdamWGroup(offsets, buffers["numel"], buffers["step"],
+                                           *(buffers.get(n) for n in ("exp_avg", "exp_avg_sq", "exp_avg_scale",
+                                                                      "exp_avg_sq_scale"))) if ext else None)
         for i, (p, at) in enumerate(zip(params, offsets)):
             n, state = p.numel(), {"step": buffers["step"][i]}
             for name in ("exp_avg", "exp_avg_sq"):
@@ -102,7 +107,6 @@ class AdamW(torch.optim.Optimizer):
                     state[name] = buffers[name][at:at + n].as_strided(p.shape, p.stride())
             self.state[p] = state
 
-    @torch.no_grad()
     def step(self, closure=None, grad_scale=None):
         """One step. grad_scale: a float32 GPU tensor of one element that every gradient is multiplied with (to undo
         a loss scale, or to clip), or None."""
@@ -110,11 +114,19 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+        if not any(g["params"] for g in self.param_groups):
+            return loss
+        if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("an AdamW step cannot be captured: the bias corrections of its step would be replayed")
-        self._step(grad_scale)
+        ext = autograd._block
+        if not (ext and all(self._native) and
+                ext.adamw_step(self._native, [g["params"] for g in self.param_groups],
+                               [_hyperparameters(g) for g in self.param_groups], self.state_bits, self.seed & _M32,
+                               grad_scale)):
+            self._step(grad_scale)
         return loss
 
+    @torch.no_grad()
     def _step(self, grad_scale):
         device, taken, calls = None, [], {}  # calls: by the parameters' type, (groups, tensors)
         for index, (group, buffers) in enumerate(zip(self.param_groups, self._buffers)):
@@ -146,9 +158,10 @@ class AdamW(torch.optim.Optimizer):
             if grad_scale.numel() != 1:
                 raise ValueError(f"grad_scale must have one element, got shape {tuple(grad_scale.shape)}")
         stream = binding._stream(device)
-        for code, (groups, tensors) in calls.items():
-            binding._check(binding.wtconv_adamw_step(groups, tensors, code, self.state_bits,
-                                                     binding._ptr(grad_scale), stream))
+        with binding._on(device):
+            for code, (groups, tensors) in calls.items():
+                binding._check(binding.wtconv_adamw_step(groups, tensors, code, self.state_bits,
+                                                         binding._ptr(grad_scale), stream))
         for steps, i, _, _ in taken:
             steps[i] += 1
         torch.autograd.graph.increment_version([p for _, _, p, _ in taken])

@@ -215,6 +215,28 @@ def test_unaligned_and_channels_last_parameters(bits, dtype):
         assert torch.equal(dense[1].detach(), last.detach())
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_the_native_host_path_is_the_python_one(bits, monkeypatch):
+    """The same library calls, so the same bits, whichever path takes the step."""
+    from paper_2608_10805_amd import autograd
+
+    runs = []
+    for native in (True, False):
+        ps = make(SHAPES) + make(SHAPES[3:7], "bf16", seed=1)
+        ps[4].grad = None
+        opt = optim.AdamW([{"params": ps[:5]}, {"params": ps[5:], "lr": 0.3}], lr=LR, state_bits=bits, seed=8)
+        assert autograd._block and all(opt._native)
+        if native:
+            monkeypatch.setattr(opt, "_step", lambda scale: pytest.fail("left to Python"))
+        else:
+            opt._native = [None] * 2
+        for _ in range(2):
+            opt.step(grad_scale=torch.tensor(0.5, device=DEV))
+        runs.append([p.detach().clone() for p in ps] + [t for pair in opt.moments() for t in pair] +
+                    [opt.state[p]["step"].clone() for p in ps])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
 def test_parameters_without_gradients_are_left_alone():
     ps = make([(100,), (100,), (100,)])
     ps[1].grad = None

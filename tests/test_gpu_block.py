@@ -55,7 +55,7 @@ def check_norm(x, dy, w, b, layout, dtype, eps=1e-6):
     # the largest value, the row sums (spread over lanes) stay below 64 + C / 16 roundings
     row = 64 + C / 16
     ref.close(y, want_y, dtype, row)
-    ref.close(got[0], want_dx, dtype, row, scale=float((dy.float().abs().max() * rstd.max() * (w.abs().max() if w is not None else 1))))
+    ref.close(got[0], want_dx, dtype, row, scale=float(dy.float().abs().max() * rstd.max() * (w.detach().abs().max() if w is not None else 1)))
     if w is not None:
         # sums over all pixels of products near 1: a rounding of each term's size and of the running sum's
         n = max(1, x.numel() // C)
@@ -392,6 +392,96 @@ def test_residual_gradient_against_differences():
             down, lo = f(), flat[i].item()
             flat[i] = old
             assert abs((up - down) / (hi - lo) - g.view(-1)[i].item()) < 60 * 8 * 2.0 ** -22
+
+
+# ----------------------------------------------------------------------------
+# the native host path against the Python one: the same library calls, so the
+# same bits, and the cases it leaves to Python
+# ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+@pytest.mark.parametrize("params", ["both", "weight", "bias", "none"])
+@pytest.mark.parametrize("need_x", [True, False])
+def test_native_norm_is_the_python_one(layout, params, need_x):
+    x, dy, w, b = norm_problem(layout, 2, 24, (5, 7), "bf16")
+    assert autograd.load_block(x), "the native host path is not built"
+    x.requires_grad_(need_x)
+    w = w.requires_grad_(True) if params in ("both", "weight") else None
+    b = b.requires_grad_(True) if params in ("both", "bias") else None
+    leaves = [t for t in (x, w, b) if t is not None and t.requires_grad]
+    args = (x, w, b, 1e-6, *LAYOUTS[layout])
+    assert autograd._block.layer_norm(*args) is not None
+    fns = (autograd.layer_norm, autograd.LayerNormFunction.apply)
+    got, want = ((y, *(torch.autograd.grad(y, leaves, dy) if leaves else ())) for y in (fn(*args) for fn in fns))
+    assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want))
+    with torch.no_grad():
+        assert torch.equal(autograd.layer_norm(*args), want[0])
+    if leaves:  # an upstream gradient in another order
+        odd = dy.transpose(1, 2).contiguous().transpose(1, 2)
+        assert torch.equal(torch.autograd.grad(autograd.layer_norm(*args), leaves[0], odd)[0], want[1])
+
+
+@pytest.mark.parametrize("given", ["all", "gamma", "keep", "none"])
+def test_native_residual_is_the_python_one(given):
+    x, z, dy, gamma, keep = residual_problem(3, 20, (5, 7), "f16")
+    gamma = gamma.requires_grad_(True) if given in ("all", "gamma") else None
+    keep = keep if given in ("all", "keep") else None
+    assert autograd._block.scaled_residual(x, z, gamma, keep) is not None
+    for need in ((True, True), (False, True), (True, False), (False, False)):
+        x.requires_grad_(need[0])
+        z.requires_grad_(need[1])
+        leaves = [t for t in (x, z, gamma) if t is not None and t.requires_grad]
+        fns = (autograd.scaled_residual, autograd.ScaledResidualFunction.apply)
+        got, want = ((y, *(torch.autograd.grad(y, leaves, dy) if leaves else ()))
+                     for y in (fn(x, z, gamma, keep) for fn in fns))
+        assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+class Tagged(torch.Tensor):
+    """A subclass with torch functions of its own and no dispatch."""
+
+
+def test_other_cases_take_the_python_path():
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Count(TorchDispatchMode):
+        n = 0
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            self.n += 1
+            return func(*args, **(kwargs or {}))
+
+    x, dy, w, b = norm_problem("turned", 2, 24, (5, 7), "f32")
+    rows = x.movedim(1, -1).contiguous()
+    ext = autograd._block
+    for t in (x.transpose(2, 3), x.double(), x[:0], x.as_subclass(Tagged), x.cpu()):
+        assert ext.layer_norm(t, w, b, 1e-6, 1, -1) is None
+        assert ext.scaled_residual(t, rows, w, None) is None
+    assert ext.layer_norm(x, w.half(), b, 1e-6, 1, -1) is None and ext.layer_norm(x, w, b, 1, 1, -1) is None
+    assert ext.layer_norm(x, w, b[1:], 1e-6, 1, -1) is None and ext.layer_norm(x, w, b, 1e-6, 0, -1) is None
+    assert ext.scaled_residual(x, rows[:1], w, None) is None and ext.scaled_residual(x, rows.half(), w, None) is None
+    want = autograd.layer_norm(x, w, b, 1e-6, 1, -1)
+    tagged = autograd.layer_norm(x.as_subclass(Tagged), w, b, 1e-6, 1, -1)
+    assert type(tagged) is Tagged and torch.equal(tagged.as_subclass(torch.Tensor), want)
+    with Count() as mode:
+        assert torch.equal(autograd.layer_norm(x, w, b, 1e-6, 1, -1), want)
+        assert torch.equal(autograd.scaled_residual(x, rows, w), autograd.ScaledResidualFunction.apply(x, rows, w, None))
+    assert mode.n > 0
+    for fn in (lambda v: autograd.layer_norm(v, w, b, 1e-6, 1, -1), lambda v: autograd.scaled_residual(v, rows, w)):
+        with pytest.raises(Exception):  # forward-mode is refused, not ignored
+            torch.func.jvp(fn, (x,), (x,))
+        with pytest.raises(Exception):  # so is vmap
+            torch.vmap(fn)(x[None])
+
+
+def test_saved_tensor_hooks_see_the_saved_tensors():
+    x, dy, w, b = norm_problem("rows", 2, 24, 35, "f32")
+    x.requires_grad_(True)
+    want = torch.autograd.grad(autograd.layer_norm(x, w, b), x, dy)[0]
+    seen = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda v: (seen.append(v.shape), v)[1], lambda v: v.clone()):
+        y = autograd.layer_norm(x, w, b)
+    assert torch.equal(torch.autograd.grad(y, x, dy)[0], want) and len(seen) == 3
 
 
 # ----------------------------------------------------------------------------
