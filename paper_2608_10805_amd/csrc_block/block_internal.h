@@ -67,6 +67,12 @@ static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
 int64_t norm_parts(const wtconv_norm_desc& d);      // rows of partial sums of the backward
 int64_t residual_parts(const wtconv_residual_desc& d);
 
+// The kernels that hold every channel of a pixel in registers; false, with
+// nothing launched, where there are too many.
+bool launch_rows_forward(wtconv_dtype dt, const NormArgs& a, hipStream_t s);
+bool launch_rows_backward(wtconv_dtype dt, const NormArgs& a, hipStream_t s);
+bool launch_planes_forward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s);
+bool launch_planes_backward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_forward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_backward(const wtconv_norm_desc& d, NormArgs a, float* dw, float* db, hipStream_t s);
 hipError_t launch_residual_forward(wtconv_dtype dt, const ResidualArgs& a, hipStream_t s);

@@ -1,6 +1,6 @@
-// Layer norm over the channels of each pixel, forward and backward.
-#include "block_internal.h"
-#include "wtconv_device.h"
+// Layer norm over the channels of each pixel, forward and backward: the
+// kernels for any number of channels, and which kernels run.
+#include "norm_device.h"
 
 namespace wtc {
 namespace {
@@ -244,18 +244,26 @@ __global__ void __launch_bounds__(kThreads) planes_sums_any(const NormArgs a)
     }
 }
 
-// The sums of the rows of partial sums, in their order: 64 columns a workgroup,
-// every fourth row a wavefront.
+// The sums of the rows of partial sums, in a fixed order: 16 columns a
+// workgroup, every 16th row a thread, several rows on their way at once.
+constexpr int kColumns = 16, kRows = kThreads / kColumns;
+
 __global__ void __launch_bounds__(kThreads)
 sum_parts_kernel(const float* part, int64_t rows, int width, int half, float* out, float* out2)
 {
-    __shared__ float red[4][kTile];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = blockIdx.x * kTile + lane;
+    __shared__ float red[kRows][kColumns + 1];
+    const int col = threadIdx.x % kColumns, row = threadIdx.x / kColumns, i = blockIdx.x * kColumns + col;
     float s = 0.f;
-    if (i < width)
-        for (int64_t r = w; r < rows; r += 4) s += part[r * width + i];
-    s = tile_sum(s, red);
-    if (w || i >= width) return;
+    if (i < width) {
+#pragma unroll 8
+        for (int64_t r = row; r < rows; r += kRows) s += part[r * width + i];
+    }
+    red[row][col] = s;
+    __syncthreads();
+    if (row || i >= width) return;
+    s = 0.f;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) s += red[r][col];
     if (i < half) {
         if (out) out[i] = s;
     } else if (out2) {
@@ -263,15 +271,13 @@ sum_parts_kernel(const float* part, int64_t rows, int width, int half, float* ou
     }
 }
 
-int grid_for(int64_t items, int64_t most) { return (int)(items < most ? (items > 1 ? items : 1) : most); }
-
 template <typename T>
 hipError_t forward_t(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s)
 {
     if (d.in == WTCONV_ROWS) {
-        hipLaunchKernelGGL(rows_forward_any<T>, dim3(grid_for((a.N + 3) / 4, 1 << 16)), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL(rows_forward_any<T>, dim3(at_most((a.N + 3) / 4, 1 << 16)), dim3(kThreads), 0, s, a);
     } else {
-        const dim3 grid(grid_for((a.N + kTile - 1) / kTile, 1 << 16));
+        const dim3 grid(at_most((a.N + kTile - 1) / kTile, 1 << 16));
         if (d.out == WTCONV_PLANES)
             hipLaunchKernelGGL((planes_forward_any<T, true>), grid, dim3(kThreads), 0, s, a);
         else
@@ -286,10 +292,10 @@ hipError_t backward_t(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t 
     const dim3 sums((a.C + kTile - 1) / kTile, a.nparts);
     if (d.in == WTCONV_ROWS) {
         if (a.out)
-            hipLaunchKernelGGL(rows_backward_any<T>, dim3(grid_for((a.N + 3) / 4, 1 << 16)), dim3(kThreads), 0, s, a);
+            hipLaunchKernelGGL(rows_backward_any<T>, dim3(at_most((a.N + 3) / 4, 1 << 16)), dim3(kThreads), 0, s, a);
         if (a.part) hipLaunchKernelGGL(rows_sums_any<T>, sums, dim3(kThreads), 0, s, a);
     } else {
-        const dim3 grid(grid_for((a.N + kTile - 1) / kTile, 1 << 16));
+        const dim3 grid(at_most((a.N + kTile - 1) / kTile, 1 << 16));
         if (d.out == WTCONV_PLANES) {
             if (a.out) hipLaunchKernelGGL((planes_backward_any<T, true>), grid, dim3(kThreads), 0, s, a);
             if (a.part) hipLaunchKernelGGL((planes_sums_any<T, true>), sums, dim3(kThreads), 0, s, a);
@@ -305,20 +311,21 @@ hipError_t backward_t(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t 
 
 int64_t norm_parts(const wtconv_norm_desc& d)
 {
-    const int64_t tiles = (d.B * d.S + kTile - 1) / kTile;
-    return grid_for(tiles, 128);
+    return at_most((d.B * d.S + 15) / 16, 1024);
 }
 
 hipError_t launch_sum_parts(const float* part, int64_t rows, int width, int half, float* out, float* out2,
                             hipStream_t s)
 {
-    hipLaunchKernelGGL(sum_parts_kernel, dim3((width + kTile - 1) / kTile), dim3(kThreads), 0, s, part, rows, width,
+    hipLaunchKernelGGL(sum_parts_kernel, dim3((width + kColumns - 1) / kColumns), dim3(kThreads), 0, s, part, rows, width,
                        half, out, out2);
     return hipGetLastError();
 }
 
 hipError_t launch_norm_forward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s)
 {
+    if (d.in == WTCONV_ROWS ? launch_rows_forward(d.dtype, a, s) : launch_planes_forward(d, a, s))
+        return hipGetLastError();
     switch (d.dtype) {
         case WTCONV_F32: return forward_t<float>(d, a, s);
         case WTCONV_BF16: return forward_t<uint16_t>(d, a, s);
@@ -330,10 +337,14 @@ hipError_t launch_norm_forward(const wtconv_norm_desc& d, const NormArgs& a, hip
 hipError_t launch_norm_backward(const wtconv_norm_desc& d, NormArgs a, float* dw, float* db, hipStream_t s)
 {
     hipError_t e = hipErrorInvalidValue;
-    switch (d.dtype) {
-        case WTCONV_F32: e = backward_t<float>(d, a, s); break;
-        case WTCONV_BF16: e = backward_t<uint16_t>(d, a, s); break;
-        case WTCONV_F16: e = backward_t<_Float16>(d, a, s); break;
+    if (d.in == WTCONV_ROWS ? launch_rows_backward(d.dtype, a, s) : launch_planes_backward(d, a, s)) {
+        e = hipGetLastError();
+    } else {
+        switch (d.dtype) {
+            case WTCONV_F32: e = backward_t<float>(d, a, s); break;
+            case WTCONV_BF16: e = backward_t<uint16_t>(d, a, s); break;
+            case WTCONV_F16: e = backward_t<_Float16>(d, a, s); break;
+        }
     }
     if (e != hipSuccess || !a.part) return e;
     return launch_sum_parts(a.part, a.nparts, 2 * a.C, a.C, dw, db, s);
