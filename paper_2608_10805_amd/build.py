@@ -20,8 +20,8 @@ LIB = os.path.join(HERE, "libwtconv.so")
 SOURCES = ["wtconv_api.cpp", "wtconv_noalloc.cpp", "wtconv_fwd.hip", "wtconv_mixed.hip", "wtconv_bwd.hip",
            "wtconv_bwd9.hip", "wtconv_phase_fwd.hip", "wtconv_phase_grad.hip", "wtconv_grad.hip",
            "wtconv_kernels.hip", "wtconv_tiny.hip"]
-BLOCK_SOURCES = ["block_api.cpp", "norm.hip", "norm_planes_fwd.hip", "norm_planes_bwd.hip", "norm_rows.hip",
-                 "residual.hip", "adamw.hip"]
+BLOCK_SOURCES = ["block_api.cpp", "norm.hip", "norm_planes_f32.hip", "norm_planes_bf16.hip",
+                 "norm_planes_f16.hip", "norm_rows.hip", "residual.hip", "adamw.hip"]
 # measurement helper used only by the benchmark (sustained VALU rate)
 PROBE_LIB = os.path.join(HERE, "libvalu_probe.so")
 PROBE_SOURCES = ["valu_probe.hip"]

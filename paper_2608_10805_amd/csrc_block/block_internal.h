@@ -71,8 +71,9 @@ int64_t residual_parts(const wtconv_residual_desc& d);
 // nothing launched, where there are too many.
 bool launch_rows_forward(wtconv_dtype dt, const NormArgs& a, hipStream_t s);
 bool launch_rows_backward(wtconv_dtype dt, const NormArgs& a, hipStream_t s);
-bool launch_planes_forward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s);
-bool launch_planes_backward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s);
+bool launch_planes_f32(bool forward, bool out_planes, const NormArgs& a, hipStream_t s);
+bool launch_planes_bf16(bool forward, bool out_planes, const NormArgs& a, hipStream_t s);
+bool launch_planes_f16(bool forward, bool out_planes, const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_forward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_backward(const wtconv_norm_desc& d, NormArgs a, float* dw, float* db, hipStream_t s);
 hipError_t launch_residual_forward(wtconv_dtype dt, const ResidualArgs& a, hipStream_t s);

@@ -307,6 +307,17 @@ hipError_t backward_t(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t 
     return hipGetLastError();
 }
 
+bool launch_planes(bool forward, const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s)
+{
+    const bool out_planes = d.out == WTCONV_PLANES;
+    switch (d.dtype) {
+        case WTCONV_F32: return launch_planes_f32(forward, out_planes, a, s);
+        case WTCONV_BF16: return launch_planes_bf16(forward, out_planes, a, s);
+        case WTCONV_F16: return launch_planes_f16(forward, out_planes, a, s);
+    }
+    return false;
+}
+
 }  // namespace
 
 int64_t norm_parts(const wtconv_norm_desc& d)
@@ -324,7 +335,7 @@ hipError_t launch_sum_parts(const float* part, int64_t rows, int width, int half
 
 hipError_t launch_norm_forward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s)
 {
-    if (d.in == WTCONV_ROWS ? launch_rows_forward(d.dtype, a, s) : launch_planes_forward(d, a, s))
+    if (d.in == WTCONV_ROWS ? launch_rows_forward(d.dtype, a, s) : launch_planes(true, d, a, s))
         return hipGetLastError();
     switch (d.dtype) {
         case WTCONV_F32: return forward_t<float>(d, a, s);
@@ -337,7 +348,7 @@ hipError_t launch_norm_forward(const wtconv_norm_desc& d, const NormArgs& a, hip
 hipError_t launch_norm_backward(const wtconv_norm_desc& d, NormArgs a, float* dw, float* db, hipStream_t s)
 {
     hipError_t e = hipErrorInvalidValue;
-    if (d.in == WTCONV_ROWS ? launch_rows_backward(d.dtype, a, s) : launch_planes_backward(d, a, s)) {
+    if (d.in == WTCONV_ROWS ? launch_rows_backward(d.dtype, a, s) : launch_planes(false, d, a, s)) {
         e = hipGetLastError();
     } else {
         switch (d.dtype) {

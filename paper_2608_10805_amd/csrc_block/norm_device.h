@@ -29,6 +29,57 @@ DEV void store_pack(T* p, const float (&f)[V])
     *reinterpret_cast<Pack<T, V>*>(p) = q;
 }
 
+// Value of the lane that the DPP control names (within 16 lanes).
+template <int CTRL>
+DEV float from_lane(float v)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+
+// v plus its value 16 or 32 lanes away (the lanes' number with that bit turned).
+DEV float add_16(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+DEV float add_32(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Sum over the lanes whose number is the same modulo LP, in each of them: by
+// rotations within 16 lanes (each step's values repeat at the last one's
+// distance), then across the rows of 16.
+template <int LP>
+DEV float sum_beyond(float v)
+{
+    if constexpr (LP <= 8) v += from_lane<0x128>(v);
+    if constexpr (LP <= 4) v += from_lane<0x124>(v);
+    if constexpr (LP <= 2) v += from_lane<0x122>(v);
+    if constexpr (LP <= 1) v += from_lane<0x121>(v);
+    if constexpr (LP <= 16) v = add_16(v);
+    if constexpr (LP <= 32) v = add_32(v);
+    return v;
+}
+
+// Sum over each group of `n` lanes side by side, a power of two, in each of them.
+DEV float sum_within(float v, int n)
+{
+    if (n > 1) v += from_lane<0xb1>(v);   // quad_perm 1 0 3 2
+    if (n > 2) v += from_lane<0x4e>(v);   // quad_perm 2 3 0 1
+    if (n > 4) v += from_lane<0x141>(v);  // row_half_mirror
+    if (n > 8) v += from_lane<0x140>(v);  // row_mirror
+    if (n > 16) v = add_16(v);
+    if (n > 32) v = add_32(v);
+    return v;
+}
+
+// Workgroups go round the 8 XCDs, each with an L2 of its own: the number of this
+// workgroup among `n` (a multiple of 8) such that the ones on an XCD follow each
+// other, and tiles that share lines of memory share an L2.
+DEV uint32_t follow(uint32_t block, uint32_t n) { return (block & 7) * (n >> 3) + (block >> 3); }
+
 inline int at_most(int64_t items, int64_t most) { return (int)(items < most ? (items > 1 ? items : 1) : most); }
 
 }  // namespace wtc

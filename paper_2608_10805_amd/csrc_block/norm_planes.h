@@ -1,170 +1,347 @@
-// Layer norm of planes with the channels of a tile of pixels in registers.
+// Layer norm of planes with the channels of a tile of pixels in registers: one
+// read and one write of every element.
 //
 // A workgroup takes P pixels and all C channels. LP lanes side by side hold V
 // adjacent pixels each (P = LP * V), so that every load is a run of P pixels of
-// one channel; slot s = thread / LP holds the channels s, s + NS, ... of them,
-// at most K. Each value is read once. The sums over the channels go lane by
-// lane over the K values, across the slots of a wavefront, and across the
-// wavefronts through LDS. Rows (the output of the forward pass, dy of the
-// backward pass) are turned in LDS, `chunk` channels at a time, with rows an
-// odd number of words apart so that neither side meets its own banks.
+// one channel; slot s = thread / LP holds the channels (k * NS + s) * G to + G
+// for k < K. The sums over the channels go over a lane's values, across the
+// slots of a wavefront, and across the wavefronts through LDS. Rows (the output
+// of the forward pass, dy of the backward pass) are turned in LDS (turn.h). The
+// backward pass keeps the weight's and bias's gradients of its channels in
+// registers over all of its workgroup's tiles.
+//
+// Bound by memory.
 #pragma once
 
-#include "norm_device.h"
+#include "turn.h"
 
 namespace wtc {
 
-template <int TH_, int V_, int LP_, int K_>
-struct PlanesShape {
-    static constexpr int TH = TH_, V = V_, LP = LP_, K = K_;
-    static constexpr int P = LP * V, NS = TH / LP, NW = TH / 64;
-    static constexpr int kMaxC = NS * K;
-};
-
-constexpr int kTurnBytes = 32 * 1024;  // LDS that turns rows: leaves room for four workgroups a CU and more
-
-// Elements between two rows in LDS: an odd number of words, at least `width` elements.
-template <typename T>
-__host__ __device__ constexpr int turn_stride(int width)
-{
-    constexpr int per = 4 / sizeof(T);
-    const int words = (width + per - 1) / per;
-    return (words | 1) * per;
-}
-
-// Slots' values that are turned at once: chunk channels = slots * (this many).
-template <typename T, typename Sh>
-__host__ __device__ constexpr int turn_steps()
-{
-    int n = Sh::K;
-    while (n > 1 && Sh::P * turn_stride<T>(n * Sh::NS) * (int)sizeof(T) > kTurnBytes) --n;
-    return n;
-}
-
-template <typename T, typename Sh>
-constexpr int turn_elements()
-{
-    return Sh::P * turn_stride<T>(turn_steps<T, Sh>() * Sh::NS);
-}
-
 // The sum of s over all slots, for this lane's pixels.
-template <typename Sh>
-DEV void slot_sum(float (&s)[Sh::V], float (*red)[Sh::P])
+template <typename Ti>
+DEV void slot_sum(float (&s)[Ti::V], float (*red)[Ti::P])
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, px = threadIdx.x % Sh::LP;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, px = threadIdx.x % Ti::LP;
 #pragma unroll
-    for (int v = 0; v < Sh::V; ++v)
+    for (int v = 0; v < Ti::V; ++v) s[v] = sum_beyond<Ti::LP>(s[v]);
+    if (lane < Ti::LP)
 #pragma unroll
-        for (int o = Sh::LP; o < 64; o <<= 1) s[v] += __shfl_xor(s[v], o);
-    if (lane < Sh::LP)
-#pragma unroll
-        for (int v = 0; v < Sh::V; ++v) red[w][px * Sh::V + v] = s[v];
+        for (int v = 0; v < Ti::V; ++v) red[w][px * Ti::V + v] = s[v];
     __syncthreads();
 #pragma unroll
-    for (int v = 0; v < Sh::V; ++v) {
+    for (int v = 0; v < Ti::V; ++v) {
         s[v] = 0.f;
 #pragma unroll
-        for (int i = 0; i < Sh::NW; ++i) s[v] += red[i][px * Sh::V + v];
+        for (int i = 0; i < Ti::NW; ++i) s[v] += red[i][px * Ti::V + v];
     }
 }
 
-// Calls f(row, column, element of the tile) for the count x width elements of
-// consecutive rows, two adjacent columns at once for 16-bit types if `pairs`.
-template <int TH, int STEP, typename F>
-DEV void over_rows(int count, int width, F&& f)
+// f[g] = p[c + g], or `none` without p or past C.
+template <int G>
+DEV void load_channels(const float* p, int c, int C, float none, float (&f)[G])
 {
-    const int per = width / STEP;
-    const uint32_t magic = 0xffffffffu / (uint32_t)per + 1u;  // exact for products below 2^32 / width
-    for (int i = threadIdx.x; i < count * per; i += TH) {
-        const int r = per == 1 ? i : (int)__umulhi((uint32_t)i, magic);
-        f(r, (i - r * per) * STEP);
-    }
-}
-
-// Copies `count` rows of `width` channels from c0 on between memory (rows
-// `pitch` apart) and LDS (rows `stride` apart).
-template <bool OUT, int TH, typename T, typename U>
-DEV void turn_rows(U* mem, int64_t pitch, T* turn, int stride, int count, int width, int c0, bool pairs)
-{
-    if (sizeof(T) == 2 && pairs) {
-        over_rows<TH, 2>(count, width, [&](int r, int c) {
-            auto* m = reinterpret_cast<std::conditional_t<OUT, uint32_t, const uint32_t>*>(mem + r * pitch + c0 + c);
-            auto* t = reinterpret_cast<uint32_t*>(turn + r * stride + c);
-            if constexpr (OUT)
-                *m = *t;
-            else
-                *t = *m;
-        });
-    } else {
-        over_rows<TH, 1>(count, width, [&](int r, int c) {
-            if constexpr (OUT)
-                mem[r * pitch + c0 + c] = turn[r * stride + c];
-            else
-                turn[r * stride + c] = mem[r * pitch + c0 + c];
-        });
-    }
-}
-
-// First element of pixel q of planes.
-DEV int64_t pixel_at(const NormArgs& a, int64_t q)
-{
-    const int64_t b = q / a.S;
-    return b * a.C * a.S + (q - b * a.S);
-}
-
-// The shapes by number of channels, smallest tile of values first; a shape is
-// chosen by pick_planes().
-template <int V, typename F>
-bool planes_shape(int index, F&& f)
-{
-    if constexpr (V == 4) {
-        switch (index) {
-            case 0: f(PlanesShape<256, 4, 16, 6>{}); return true;
-            case 1: f(PlanesShape<256, 4, 16, 12>{}); return true;
-            case 2: f(PlanesShape<256, 4, 8, 6>{}); return true;
-            case 3: f(PlanesShape<256, 4, 8, 12>{}); return true;
-            case 4: f(PlanesShape<256, 4, 4, 6>{}); return true;
-            case 5: f(PlanesShape<256, 4, 4, 12>{}); return true;
-            case 6: f(PlanesShape<512, 4, 4, 16>{}); return true;
+    struct Quad { float v[4]; };
+    if (p && c + G <= C) {
+#pragma unroll
+        for (int g = 0; g < G; g += 4) {
+            const Quad q = *reinterpret_cast<const Quad*>(p + c + g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[g + i] = q.v[i];
         }
     } else {
-        switch (index) {
-            case 0: f(PlanesShape<256, 1, 64, 12>{}); return true;
-            case 1: f(PlanesShape<256, 1, 64, 24>{}); return true;
-            case 2: f(PlanesShape<256, 1, 32, 12>{}); return true;
-            case 3: f(PlanesShape<256, 1, 32, 24>{}); return true;
-            case 4: f(PlanesShape<256, 1, 16, 12>{}); return true;
-            case 5: f(PlanesShape<256, 1, 16, 24>{}); return true;
-            case 6: f(PlanesShape<512, 1, 16, 24>{}); return true;
-            case 7: f(PlanesShape<512, 1, 8, 32>{}); return true;
+#pragma unroll
+        for (int g = 0; g < G; ++g) f[g] = p && c + g < C ? p[c + g] : none;
+    }
+}
+
+template <typename Ti, bool OUT_PLANES>
+__global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const Pixels ps)
+{
+    using T = typename Ti::Type;
+    using Tu = Turn<Ti>;
+    constexpr int V = Ti::V, NS = Ti::NS, K = Ti::K, G = Ti::G;
+    constexpr bool kShared = Ti::P * sizeof(T) < 128;  // tiles side by side share lines of memory
+    __shared__ float red[2][Ti::NW][Ti::P];
+    __shared__ uint4 turn[OUT_PLANES ? 1 : Tu::kSize];
+    const int px = threadIdx.x % Ti::LP, slot = threadIdx.x / Ti::LP;
+    const int64_t q0 = (int64_t)(kShared ? follow(blockIdx.x, gridDim.x) : blockIdx.x) * Ti::P, q = q0 + px * V;
+    if (q0 >= a.N) return;
+    const bool in = q < a.N;  // (a vector lies within one image)
+    const Place<Ti> at(ps, (uint32_t)q0, (uint32_t)(in ? q : q0), slot);
+    float v[K][V][G], s[V] = {}, mean[V], rstd[V];
+    int left[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        left[k] = in ? a.C - (k * NS + slot) * G : 0;
+        load_pixels<Ti>((const T*)a.x, at, ps, left[k], k, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        over_channels<Ti>(left[k], [&](int g) ALWAYS {
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[i] += v[k][i][g];
+        });
+    slot_sum<Ti>(s, red[0]);
+    const float per = 1.0f / a.C;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        mean[i] = s[i] * per;
+        s[i] = 0.f;
+    }
+    // the variance from the centred values, which are at hand: no cancellation
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        over_channels<Ti>(left[k], [&](int g) ALWAYS {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[k][i][g] -= mean[i];
+                s[i] += v[k][i][g] * v[k][i][g];
+            }
+        });
+    slot_sum<Ti>(s, red[1]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) rstd[i] = 1.0f / sqrtf(s[i] * per + a.eps);
+    if (a.mean && in && slot == 0)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            a.mean[q + i] = mean[i];
+            a.rstd[q + i] = rstd[i];
+        }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (left[k] <= 0) continue;
+        float w[G], b[G];
+        load_channels<G>(a.w, (k * NS + slot) * G, a.C, 1.0f, w);
+        load_channels<G>(a.b, (k * NS + slot) * G, a.C, 0.0f, b);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int g = 0; g < G; ++g) v[k][i][g] = v[k][i][g] * rstd[i] * w[g] + b[g];
+        if (OUT_PLANES) store_pixels<Ti>((T*)a.out, at, ps, left[k], k, v[k]);
+    }
+    if constexpr (!OUT_PLANES) {
+        const int rows = a.N - q0 < Ti::P ? (int)(a.N - q0) : Ti::P;
+#pragma unroll
+        for (int k0 = 0; k0 < K; k0 += Tu::kSteps) {
+            const int c0 = k0 * Ti::kChannels;
+            if (c0 >= a.C) break;
+            if (k0) __syncthreads();
+#pragma unroll
+            for (int k = k0; k < k0 + Tu::kSteps && k < K; ++k)
+                if (left[k] > 0) Tu::put(turn, px, (k - k0) * NS + slot, v[k]);
+            __syncthreads();
+            Tu::template copy<true>((T*)a.out + q0 * a.C + c0, a.C, turn, rows,
+                                    a.C - c0 < Tu::kWidth ? a.C - c0 : Tu::kWidth);
         }
     }
+}
+
+template <typename Ti, bool OUT_PLANES>
+__global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, const Pixels ps)
+{
+    using T = typename Ti::Type;
+    using Tu = Turn<Ti>;
+    constexpr int V = Ti::V, NS = Ti::NS, K = Ti::K, G = Ti::G;
+    constexpr bool kShared = Ti::P * sizeof(T) < 128;  // tiles side by side share lines of memory
+    __shared__ float red[2][Ti::NW][Ti::P];
+    __shared__ uint4 turn[OUT_PLANES ? 1 : Tu::kSize];
+    const int px = threadIdx.x % Ti::LP, slot = threadIdx.x / Ti::LP;
+    const float per = 1.0f / a.C;
+    float sw[K][G] = {}, sb[K][G] = {};
+    const uint32_t first = !kShared || gridDim.x % 8 ? blockIdx.x : follow(blockIdx.x, gridDim.x);
+    for (int64_t q0 = (int64_t)first * Ti::P; q0 < a.N; q0 += (int64_t)gridDim.x * Ti::P) {
+        const int64_t q = q0 + px * V;
+        const bool in = q < a.N;
+        const Place<Ti> at(ps, (uint32_t)q0, (uint32_t)(in ? q : q0), slot);
+        float xhat[K][V][G], g[K][V][G], s1[V] = {}, s2[V] = {}, mean[V], rstd[V];
+        int left[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            left[k] = in ? a.C - (k * NS + slot) * G : 0;
+            load_pixels<Ti>((const T*)a.x, at, ps, left[k], k, xhat[k]);
+            if (OUT_PLANES) load_pixels<Ti>((const T*)a.dy, at, ps, left[k], k, g[k]);
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            mean[i] = in ? a.mean[q + i] : 0.f;
+            rstd[i] = in ? a.rstd[q + i] : 0.f;
+        }
+        if constexpr (!OUT_PLANES) {
+            const int rows = a.N - q0 < Ti::P ? (int)(a.N - q0) : Ti::P;
+#pragma unroll
+            for (int k0 = 0; k0 < K; k0 += Tu::kSteps) {
+                const int c0 = k0 * Ti::kChannels;
+                if (c0 >= a.C) break;
+                __syncthreads();
+                Tu::template copy<false>((const T*)a.dy + q0 * a.dy_stride + c0, a.dy_stride, turn, rows,
+                                         a.C - c0 < Tu::kWidth ? a.C - c0 : Tu::kWidth);
+                __syncthreads();
+#pragma unroll
+                for (int k = k0; k < k0 + Tu::kSteps && k < K; ++k)
+                    if (left[k] > 0) Tu::get(turn, px, (k - k0) * NS + slot, g[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float w[G];
+            if (left[k] > 0) load_channels<G>(a.w, (k * NS + slot) * G, a.C, 1.0f, w);
+            over_channels<Ti>(left[k], [&](int j) ALWAYS {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    xhat[k][i][j] = (xhat[k][i][j] - mean[i]) * rstd[i];
+                    sw[k][j] += g[k][i][j] * xhat[k][i][j];
+                    sb[k][j] += g[k][i][j];
+                    g[k][i][j] *= w[j];
+                    s1[i] += g[k][i][j];
+                    s2[i] += g[k][i][j] * xhat[k][i][j];
+                }
+            });
+        }
+        if (!a.out) continue;
+        __syncthreads();  // the last tile's sums have been read
+        slot_sum<Ti>(s1, red[0]);
+        slot_sum<Ti>(s2, red[1]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            s1[i] *= per * rstd[i];
+            s2[i] *= per * rstd[i];
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            over_channels<Ti>(left[k], [&](int j) ALWAYS {
+#pragma unroll
+                for (int i = 0; i < V; ++i) g[k][i][j] = rstd[i] * g[k][i][j] - s1[i] - xhat[k][i][j] * s2[i];
+            });
+            store_pixels<Ti>((T*)a.out, at, ps, left[k], k, g[k]);
+        }
+    }
+    if (!a.part) return;
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.C;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            const int c = (k * NS + slot) * G + j;
+#pragma unroll
+            for (int o = Ti::LP >> 1; o; o >>= 1) {
+                sw[k][j] += __shfl_xor(sw[k][j], o);
+                sb[k][j] += __shfl_xor(sb[k][j], o);
+            }
+            if (px == 0 && c < a.C) {
+                part[c] = sw[k][j];
+                part[a.C + c] = sb[k][j];
+            }
+        }
+}
+
+// The tiles of a type and vector, by index.
+template <typename T, int V, bool WHOLE, typename F>
+bool planes_tile(int index, F&& f)
+{
+#define WTC_TILE(i, TH, LP, K) \
+    case i: f(Tile<T, TH, V, LP, K, WHOLE>{}); return true
+    if constexpr (sizeof(T) == 4 && V == 4) {
+        switch (index) {
+            WTC_TILE(0, 192, 16, 2);
+            WTC_TILE(1, 256, 16, 2);
+            WTC_TILE(2, 192, 8, 1);
+            WTC_TILE(3, 192, 8, 2);
+            WTC_TILE(4, 256, 8, 3);
+            WTC_TILE(5, 192, 4, 1);
+            WTC_TILE(6, 192, 4, 2);
+            WTC_TILE(7, 256, 4, 3);
+            WTC_TILE(8, 512, 4, 3);
+        }
+    } else if constexpr (V == 4) {
+        switch (index) {
+            WTC_TILE(0, 192, 16, 1);
+            WTC_TILE(1, 256, 16, 1);
+            WTC_TILE(2, 192, 8, 1);
+            WTC_TILE(3, 256, 8, 1);
+            WTC_TILE(4, 192, 4, 1);
+            WTC_TILE(5, 256, 4, 1);
+            WTC_TILE(6, 384, 4, 1);
+            WTC_TILE(7, 512, 4, 1);
+            WTC_TILE(8, 768, 4, 1);
+        }
+    } else {
+        constexpr int E = 4 / sizeof(T);  // twice the channels a unit, half the steps
+        switch (index) {
+            WTC_TILE(0, 256, 64, E == 1 ? 6 : 3);
+            WTC_TILE(1, 256, 32, E == 1 ? 6 : 3);
+            WTC_TILE(2, 256, 16, E == 1 ? 6 : 3);
+            WTC_TILE(3, 512, 16, E == 1 ? 6 : 3);
+            WTC_TILE(4, 1024, 16, E == 1 ? 6 : 3);
+        }
+    }
+#undef WTC_TILE
     return false;
 }
 
-// The shape for C channels and N pixels, or -1 where none holds them: the
-// longest runs of pixels that still leave four tiles a CU, else the shortest.
-template <int V>
-int pick_planes(int C, int64_t N)
+// The tile for C channels and N pixels, or -1 where none holds them: by the
+// share of lanes that have channels, the length of the runs of pixels (whole
+// lines of 128 bytes are best), and whether there are two tiles a CU.
+template <typename T, int V, bool WHOLE>
+int pick_tile(int C, int64_t N)
 {
-    int best = -1, best_pixels = 0, most = 0, pixels = 0;
-    for (int i = 0; planes_shape<V>(i, [&](auto sh) { most = decltype(sh)::kMaxC; pixels = decltype(sh)::P; }); ++i) {
-        if (C > most || (best >= 0 && C * 4 < most)) continue;  // (too few channels for so many slots)
-        if (N >= (int64_t)pixels * 1024) return i;
-        if (best < 0 || pixels < best_pixels) {
+    int best = -1, most = 0, pixels = 0, step = 1;
+    double best_score = 0;
+    for (int i = 0; planes_tile<T, V, WHOLE>(i, [&](auto t) {
+             most = decltype(t)::kMaxC;
+             pixels = decltype(t)::P;
+             step = decltype(t)::kChannels;
+         });
+         ++i) {
+        if (C > most) continue;
+        const double lanes = (double)C / ((C + step - 1) / step * step);
+        const int run = pixels * (int)sizeof(T);
+        const double lines = run >= 128 ? 1.0 : run >= 64 ? 0.9 : 0.6;
+        const double tiles = (double)N / pixels;
+        const double score = lanes * lines * (tiles >= 512 ? 1.0 : tiles / 512);
+        if (score > best_score) {
+            best_score = score;
             best = i;
-            best_pixels = pixels;
         }
     }
     return best;
 }
 
-// Pixels that are loaded at once: four where every image's planes begin and end
-// at a whole vector.
-inline int planes_vector(const NormArgs& a, size_t element, const void* other)
+template <typename T, int V, bool WHOLE>
+bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
 {
-    const uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.out | (uintptr_t)other;
-    return a.S % 4 == 0 && all % (4 * element) == 0 ? 4 : 1;
+    const int i = pick_tile<T, V, WHOLE>(a.C, a.N);
+    bool done = false;
+    planes_tile<T, V, WHOLE>(i, [&](auto t) {
+        using Ti = decltype(t);
+        if (!pixels_fit<Ti>(a.N, a.S, a.C)) return;
+        done = true;
+        const Pixels ps = pixels_of(a.S, a.C);
+        const unsigned tiles = (unsigned)((a.N + Ti::P - 1) / Ti::P);
+        const dim3 grid(forward ? (tiles + 7) / 8 * 8 : (unsigned)a.nparts), block(Ti::TH);
+        if (forward && out_planes)
+            hipLaunchKernelGGL((planes_forward<Ti, true>), grid, block, 0, s, a, ps);
+        else if (forward)
+            hipLaunchKernelGGL((planes_forward<Ti, false>), grid, block, 0, s, a, ps);
+        else if (out_planes)
+            hipLaunchKernelGGL((planes_backward<Ti, true>), grid, block, 0, s, a, ps);
+        else
+            hipLaunchKernelGGL((planes_backward<Ti, false>), grid, block, 0, s, a, ps);
+    });
+    return done;
+}
+
+// x and dx are planes, and y or dy if `out_planes`. Four pixels are loaded at
+// once where every image's planes begin and end at a whole vector.
+template <typename T>
+bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
+{
+    const uintptr_t all = (uintptr_t)a.x | (!forward || out_planes ? (uintptr_t)a.out : 0) |
+                          (!forward && out_planes ? (uintptr_t)a.dy : 0);
+    const bool whole = a.C % (16 / (int)sizeof(T)) == 0;
+    if (a.S % 4 == 0 && all % (4 * sizeof(T)) == 0 &&
+        (whole ? planes_launch<T, 4, true> : planes_launch<T, 4, false>)(forward, out_planes, a, s))
+        return true;
+    return (whole ? planes_launch<T, 1, true> : planes_launch<T, 1, false>)(forward, out_planes, a, s);
 }
 
 }  // namespace wtc

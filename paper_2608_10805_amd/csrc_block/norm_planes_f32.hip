@@ -1,0 +1,11 @@
+// Layer norm of planes in float32.
+#include "norm_planes.h"
+
+namespace wtc {
+
+bool launch_planes_f32(bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
+{
+    return planes_launch<float>(forward, out_planes, a, s);
+}
+
+}  // namespace wtc

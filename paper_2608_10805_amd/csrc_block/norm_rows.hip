@@ -10,12 +10,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-DEV float group_sum(float v, int gl)
-{
-    for (int o = gl >> 1; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-
 template <typename T, int V, int R>
 __global__ void __launch_bounds__(kThreads) rows_forward(const NormArgs a, int gl)
 {
@@ -38,7 +32,7 @@ __global__ void __launch_bounds__(kThreads) rows_forward(const NormArgs a, int g
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int i = 0; i < V; ++i) s += v[r][i];
-    const float per = 1.0f / a.C, mean = group_sum(s, gl) * per;
+    const float per = 1.0f / a.C, mean = sum_within(s, gl) * per;
     s = 0.f;
     // the variance from the centred values, which are at hand: no cancellation
 #pragma unroll
@@ -49,7 +43,7 @@ __global__ void __launch_bounds__(kThreads) rows_forward(const NormArgs a, int g
                 v[r][i] -= mean;
                 s += v[r][i] * v[r][i];
             }
-    const float rstd = 1.0f / sqrtf(group_sum(s, gl) * per + a.eps);
+    const float rstd = 1.0f / sqrtf(sum_within(s, gl) * per + a.eps);
     if (a.mean && lane == 0) {
         a.mean[q] = mean;
         a.rstd[q] = rstd;
@@ -104,8 +98,8 @@ __global__ void __launch_bounds__(kThreads) rows_backward(const NormArgs a, int 
                 }
         }
         if (!a.out) continue;
-        s1 = group_sum(s1, gl) * per;
-        s2 = group_sum(s2, gl) * per;
+        s1 = sum_within(s1, gl) * per;
+        s2 = sum_within(s2, gl) * per;
         T* dx = (T*)a.out + q * a.C;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
