@@ -1,5 +1,4 @@
-// What the layer norm kernels share: vectors of the storage types and sums over
-// lanes.
+// What the kernels share: vectors of the storage types and sums over lanes.
 #pragma once
 
 #include "block_internal.h"
@@ -7,26 +6,49 @@
 
 namespace wtc {
 
+// V elements. In memory they need no more than an element's alignment: the
+// copies below become whole vector loads and stores, which the hardware takes
+// from any address.
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Pack {
     T v[V];
 };
 
 template <int V, typename T>
-DEV void load_pack(const T* p, float (&f)[V])
+DEV Pack<T, V> load_pack(const T* p)
 {
-    const Pack<T, V> q = *reinterpret_cast<const Pack<T, V>*>(p);
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = to_f32(q.v[i]);
+    Pack<T, V> q;
+    __builtin_memcpy(&q, p, sizeof(q));
+    return q;
 }
 
 template <int V, typename T>
-DEV void store_pack(T* p, const float (&f)[V])
+DEV void store_pack(T* p, const Pack<T, V>& q) { __builtin_memcpy(p, &q, sizeof(q)); }
+
+// The first n elements alone, zeros after them.
+template <int V, typename T>
+DEV Pack<T, V> load_upto(const T* p, int n)
 {
     Pack<T, V> q;
+    if (n >= V) {
+        q = load_pack<V>(p);
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) q.v[i] = from_f32<T>(f[i]);
-    *reinterpret_cast<Pack<T, V>*>(p) = q;
+        for (int i = 0; i < V; ++i) q.v[i] = i < n ? p[i] : T(0);
+    }
+    return q;
+}
+
+template <int V, typename T>
+DEV void store_upto(T* p, int n, const Pack<T, V>& q)
+{
+    if (n >= V) {
+        store_pack<V>(p, q);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = q.v[i];
+    }
 }
 
 // Value of the lane that the DPP control names (within 16 lanes).

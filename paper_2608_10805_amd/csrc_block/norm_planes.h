@@ -64,16 +64,15 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     __shared__ float red[2][Ti::NW][Ti::P];
     __shared__ uint4 turn[OUT_PLANES ? 1 : Tu::kSize];
     const int px = threadIdx.x % Ti::LP, slot = threadIdx.x / Ti::LP;
-    const int64_t q0 = (int64_t)(kShared ? follow(blockIdx.x, gridDim.x) : blockIdx.x) * Ti::P, q = q0 + px * V;
-    if (q0 >= a.N) return;
-    const bool in = q < a.N;  // (a vector lies within one image)
-    const Place<Ti> at(ps, (uint32_t)q0, (uint32_t)(in ? q : q0), slot);
+    const uint32_t tile = kShared ? follow(blockIdx.x, gridDim.x) : blockIdx.x;
+    if (tile >= ps.tiles) return;
+    const Place<Ti> at(ps, tile, px, slot);
     float v[K][V][G], s[V] = {}, mean[V], rstd[V];
     int left[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        left[k] = in ? a.C - (k * NS + slot) * G : 0;
-        load_pixels<Ti>((const T*)a.x, at, ps, left[k], k, v[k]);
+        left[k] = at.left(a.C, slot, k);
+        load_pixels<Ti>((const T*)a.x, at, a.S, left[k], k, v[k]);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
@@ -85,7 +84,7 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     const float per = 1.0f / a.C;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        mean[i] = s[i] * per;
+        mean[i] = s[i] / a.C;  // (exact for a constant pixel)
         s[i] = 0.f;
     }
     // the variance from the centred values, which are at hand: no cancellation
@@ -101,12 +100,10 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     slot_sum<Ti>(s, red[1]);
 #pragma unroll
     for (int i = 0; i < V; ++i) rstd[i] = 1.0f / sqrtf(s[i] * per + a.eps);
-    if (a.mean && in && slot == 0)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            a.mean[q + i] = mean[i];
-            a.rstd[q + i] = rstd[i];
-        }
+    if (a.mean && slot == 0) {
+        store_upto<V>(a.mean + at.q, at.count, __builtin_bit_cast(Pack<float, V>, mean));
+        store_upto<V>(a.rstd + at.q, at.count, __builtin_bit_cast(Pack<float, V>, rstd));
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         if (left[k] <= 0) continue;
@@ -117,10 +114,9 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
         for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int g = 0; g < G; ++g) v[k][i][g] = v[k][i][g] * rstd[i] * w[g] + b[g];
-        if (OUT_PLANES) store_pixels<Ti>((T*)a.out, at, ps, left[k], k, v[k]);
+        if (OUT_PLANES) store_pixels<Ti>((T*)a.out, at, a.S, left[k], k, v[k]);
     }
     if constexpr (!OUT_PLANES) {
-        const int rows = a.N - q0 < Ti::P ? (int)(a.N - q0) : Ti::P;
 #pragma unroll
         for (int k0 = 0; k0 < K; k0 += Tu::kSteps) {
             const int c0 = k0 * Ti::kChannels;
@@ -130,7 +126,7 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
             for (int k = k0; k < k0 + Tu::kSteps && k < K; ++k)
                 if (left[k] > 0) Tu::put(turn, px, (k - k0) * NS + slot, v[k]);
             __syncthreads();
-            Tu::template copy<true>((T*)a.out + q0 * a.C + c0, a.C, turn, rows,
+            Tu::template copy<true>((T*)a.out + (int64_t)at.q0 * a.C + c0, a.C, turn, at.rows,
                                     a.C - c0 < Tu::kWidth ? a.C - c0 : Tu::kWidth);
         }
     }
@@ -149,31 +145,30 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
     const float per = 1.0f / a.C;
     float sw[K][G] = {}, sb[K][G] = {};
     const uint32_t first = !kShared || gridDim.x % 8 ? blockIdx.x : follow(blockIdx.x, gridDim.x);
-    for (int64_t q0 = (int64_t)first * Ti::P; q0 < a.N; q0 += (int64_t)gridDim.x * Ti::P) {
-        const int64_t q = q0 + px * V;
-        const bool in = q < a.N;
-        const Place<Ti> at(ps, (uint32_t)q0, (uint32_t)(in ? q : q0), slot);
+    for (uint32_t tile = first; tile < ps.tiles; tile += gridDim.x) {
+        const Place<Ti> at(ps, tile, px, slot);
         float xhat[K][V][G], g[K][V][G], s1[V] = {}, s2[V] = {}, mean[V], rstd[V];
         int left[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            left[k] = in ? a.C - (k * NS + slot) * G : 0;
-            load_pixels<Ti>((const T*)a.x, at, ps, left[k], k, xhat[k]);
-            if (OUT_PLANES) load_pixels<Ti>((const T*)a.dy, at, ps, left[k], k, g[k]);
+            left[k] = at.left(a.C, slot, k);
+            load_pixels<Ti>((const T*)a.x, at, a.S, left[k], k, xhat[k]);
+            if (OUT_PLANES) load_pixels<Ti>((const T*)a.dy, at, a.S, left[k], k, g[k]);
         }
+        // (a pixel that is not there: zeros, which add nothing to the sums)
+        const auto m = load_upto<V>(a.mean + at.q, at.count), r = load_upto<V>(a.rstd + at.q, at.count);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            mean[i] = in ? a.mean[q + i] : 0.f;
-            rstd[i] = in ? a.rstd[q + i] : 0.f;
+            mean[i] = m.v[i];
+            rstd[i] = r.v[i];
         }
         if constexpr (!OUT_PLANES) {
-            const int rows = a.N - q0 < Ti::P ? (int)(a.N - q0) : Ti::P;
 #pragma unroll
             for (int k0 = 0; k0 < K; k0 += Tu::kSteps) {
                 const int c0 = k0 * Ti::kChannels;
                 if (c0 >= a.C) break;
                 __syncthreads();
-                Tu::template copy<false>((const T*)a.dy + q0 * a.dy_stride + c0, a.dy_stride, turn, rows,
+                Tu::template copy<false>((const T*)a.dy + at.q0 * a.dy_stride + c0, a.dy_stride, turn, at.rows,
                                          a.C - c0 < Tu::kWidth ? a.C - c0 : Tu::kWidth);
                 __syncthreads();
 #pragma unroll
@@ -212,7 +207,7 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
 #pragma unroll
                 for (int i = 0; i < V; ++i) g[k][i][j] = rstd[i] * g[k][i][j] - s1[i] - xhat[k][i][j] * s2[i];
             });
-            store_pixels<Ti>((T*)a.out, at, ps, left[k], k, g[k]);
+            store_pixels<Ti>((T*)a.out, at, a.S, left[k], k, g[k]);
         }
     }
     if (!a.part) return;
@@ -235,11 +230,11 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
 }
 
 // The tiles of a type and vector, by index.
-template <typename T, int V, bool WHOLE, typename F>
+template <typename T, int V, bool REGULAR, typename F>
 bool planes_tile(int index, F&& f)
 {
 #define WTC_TILE(i, TH, LP, K) \
-    case i: f(Tile<T, TH, V, LP, K, WHOLE>{}); return true
+    case i: f(Tile<T, TH, V, LP, K, REGULAR>{}); return true
     if constexpr (sizeof(T) == 4 && V == 4) {
         switch (index) {
             WTC_TILE(0, 192, 16, 2);
@@ -278,25 +273,29 @@ bool planes_tile(int index, F&& f)
     return false;
 }
 
-// The tile for C channels and N pixels, or -1 where none holds them: by the
-// share of lanes that have channels, the length of the runs of pixels (whole
-// lines of 128 bytes are best), and whether there are two tiles a CU.
-template <typename T, int V, bool WHOLE>
-int pick_tile(int C, int64_t N)
+// The tile for B images of S pixels and C channels, or -1 where none holds the
+// channels: by the share of lanes that have channels and pixels, the length of
+// the runs of pixels (whole lines of 128 bytes are best), and whether there are
+// two tiles a CU.
+template <typename T, int V, bool REGULAR>
+int pick_tile(int64_t B, int64_t S, int C, double& best_score)
 {
     int best = -1, most = 0, pixels = 0, step = 1;
-    double best_score = 0;
-    for (int i = 0; planes_tile<T, V, WHOLE>(i, [&](auto t) {
-             most = decltype(t)::kMaxC;
-             pixels = decltype(t)::P;
-             step = decltype(t)::kChannels;
+    bool flat = false;
+    best_score = 0;
+    for (int i = 0; planes_tile<T, V, REGULAR>(i, [&](auto t) {
+             using Ti = decltype(t);
+             most = Ti::kMaxC;
+             pixels = Ti::P;
+             step = Ti::kChannels;
+             flat = Ti::kFlat;
          });
          ++i) {
         if (C > most) continue;
-        const double lanes = (double)C / ((C + step - 1) / step * step);
+        const double tiles = flat ? (double)(B * S + pixels - 1) / pixels : (double)B * ((S + pixels - 1) / pixels);
+        const double lanes = (double)C / ((C + step - 1) / step * step) * ((double)(B * S) / (tiles * pixels));
         const int run = pixels * (int)sizeof(T);
         const double lines = run >= 128 ? 1.0 : run >= 64 ? 0.9 : 0.6;
-        const double tiles = (double)N / pixels;
         const double score = lanes * lines * (tiles >= 512 ? 1.0 : tiles / 512);
         if (score > best_score) {
             best_score = score;
@@ -306,18 +305,16 @@ int pick_tile(int C, int64_t N)
     return best;
 }
 
-template <typename T, int V, bool WHOLE>
-bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
+template <typename T, int V, bool REGULAR>
+bool planes_launch(int index, bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
 {
-    const int i = pick_tile<T, V, WHOLE>(a.C, a.N);
     bool done = false;
-    planes_tile<T, V, WHOLE>(i, [&](auto t) {
+    planes_tile<T, V, REGULAR>(index, [&](auto t) {
         using Ti = decltype(t);
-        if (!pixels_fit<Ti>(a.N, a.S, a.C)) return;
+        Pixels ps;
+        if (!pixels_of<Ti>(a.B, a.S, a.C, ps)) return;
         done = true;
-        const Pixels ps = pixels_of(a.S, a.C);
-        const unsigned tiles = (unsigned)((a.N + Ti::P - 1) / Ti::P);
-        const dim3 grid(forward ? (tiles + 7) / 8 * 8 : (unsigned)a.nparts), block(Ti::TH);
+        const dim3 grid(forward ? (ps.tiles + 7) / 8 * 8 : (unsigned)a.nparts), block(Ti::TH);
         if (forward && out_planes)
             hipLaunchKernelGGL((planes_forward<Ti, true>), grid, block, 0, s, a, ps);
         else if (forward)
@@ -330,18 +327,20 @@ bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t
     return done;
 }
 
-// x and dx are planes, and y or dy if `out_planes`. Four pixels are loaded at
-// once where every image's planes begin and end at a whole vector.
+// x and dx are planes, and y or dy if `out_planes`. Vectors of four pixels, but
+// for images so small that most of them would be incomplete: single pixels then
+// run over all images.
 template <typename T>
 bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
 {
-    const uintptr_t all = (uintptr_t)a.x | (!forward || out_planes ? (uintptr_t)a.out : 0) |
-                          (!forward && out_planes ? (uintptr_t)a.dy : 0);
-    const bool whole = a.C % (16 / (int)sizeof(T)) == 0;
-    if (a.S % 4 == 0 && all % (4 * sizeof(T)) == 0 &&
-        (whole ? planes_launch<T, 4, true> : planes_launch<T, 4, false>)(forward, out_planes, a, s))
-        return true;
-    return (whole ? planes_launch<T, 1, true> : planes_launch<T, 1, false>)(forward, out_planes, a, s);
+    double fours = 0, ones = 0;
+    if (a.S % 4 == 0 && a.C % (16 / (int)sizeof(T)) == 0) {
+        const int i = pick_tile<T, 4, true>(a.B, a.S, a.C, fours);
+        return planes_launch<T, 4, true>(i, forward, out_planes, a, s);
+    }
+    const int i = pick_tile<T, 4, false>(a.B, a.S, a.C, fours), j = pick_tile<T, 1, false>(a.B, a.S, a.C, ones);
+    if (fours >= 0.5 * ones && planes_launch<T, 4, false>(i, forward, out_planes, a, s)) return true;
+    return planes_launch<T, 1, false>(j, forward, out_planes, a, s);
 }
 
 }  // namespace wtc

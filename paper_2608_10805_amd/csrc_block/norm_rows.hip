@@ -2,7 +2,11 @@
 // and backward: one read of every input, one write of every output.
 //
 // GL lanes (a power of two, up to a wavefront) hold a row: lane l the vectors
-// l, l + GL, ... of V elements, at most R of them. 64 / GL rows a wavefront.
+// l, l + GL, ... of V elements (16 bytes), at most R of them. 64 / GL rows a
+// wavefront. WHOLE: C is a multiple of V; else the last vector is incomplete,
+// and rows may begin at any element.
+//
+// Bound by memory.
 #include "norm_device.h"
 
 namespace wtc {
@@ -10,9 +14,25 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T, int V, int R>
+// The elements of a vector that there are: all of WHOLE rows' vectors up to C.
+template <int V, bool WHOLE>
+DEV int count_of(int c, int C) { return WHOLE ? (c < C ? V : 0) : C - c; }
+
+template <int V>
+DEV void load_columns(const float* p, int c, int n, float none, float (&f)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = none;
+    if (!p) return;
+    const Pack<float, V> q = load_upto<V>(p + c, n);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = q.v[i];
+}
+
+template <typename T, int R, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) rows_forward(const NormArgs a, int gl)
 {
+    constexpr int V = 16 / sizeof(T);
     const int lane = threadIdx.x & (gl - 1);
     const int64_t q = (int64_t)blockIdx.x * (kThreads / gl) + threadIdx.x / gl;
     if (q >= a.N) return;  // (whole groups)
@@ -21,28 +41,26 @@ __global__ void __launch_bounds__(kThreads) rows_forward(const NormArgs a, int g
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int c = (r * gl + lane) * V;
-        if (c < a.C) {
-            load_pack<V>(x + c, v[r]);
-        } else {
+        const auto p = load_upto<V>(x + c, count_of<V, WHOLE>(c, a.C));
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[r][i] = 0.f;
-        }
+        for (int i = 0; i < V; ++i) v[r][i] = to_f32(p.v[i]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int i = 0; i < V; ++i) s += v[r][i];
-    const float per = 1.0f / a.C, mean = sum_within(s, gl) * per;
+    const float per = 1.0f / a.C, mean = sum_within(s, gl) / a.C;  // (exact for a constant pixel)
     s = 0.f;
     // the variance from the centred values, which are at hand: no cancellation
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-        if ((r * gl + lane) * V < a.C)
+    for (int r = 0; r < R; ++r) {
+        const int n = count_of<V, WHOLE>((r * gl + lane) * V, a.C);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                v[r][i] -= mean;
-                s += v[r][i] * v[r][i];
-            }
+        for (int i = 0; i < V; ++i) {
+            v[r][i] = i < n ? v[r][i] - mean : 0.f;
+            s += v[r][i] * v[r][i];
+        }
+    }
     const float rstd = 1.0f / sqrtf(sum_within(s, gl) * per + a.eps);
     if (a.mean && lane == 0) {
         a.mean[q] = mean;
@@ -51,64 +69,69 @@ __global__ void __launch_bounds__(kThreads) rows_forward(const NormArgs a, int g
     T* y = (T*)a.out + q * a.C;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int c = (r * gl + lane) * V;
-        if (c < a.C) {
+        const int c = (r * gl + lane) * V, n = count_of<V, WHOLE>(c, a.C);
+        float w[V], b[V];
+        load_columns<V>(a.w, c, n, 1.0f, w);
+        load_columns<V>(a.b, c, n, 0.0f, b);
+        Pack<T, V> p;
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                v[r][i] = v[r][i] * rstd * (a.w ? a.w[c + i] : 1.0f) + (a.b ? a.b[c + i] : 0.0f);
-            store_pack<V>(y + c, v[r]);
-        }
+        for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(v[r][i] * rstd * w[i] + b[i]);
+        store_upto<V>(y + c, n, p);
     }
 }
 
 // A workgroup takes rows in steps of all workgroups' rows; each lane sums the
 // gradients of its own columns, the groups and wavefronts join at the end.
-template <typename T, int V, int R>
+template <typename T, int R, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) rows_backward(const NormArgs a, int gl)
 {
+    constexpr int V = 16 / sizeof(T);
     extern __shared__ float sums[];  // 2 C
     const int lane = threadIdx.x & (gl - 1), groups = kThreads / gl;
     const float per = 1.0f / a.C;
-    float sw[R][V] = {}, sb[R][V] = {};
+    float sw[R][V] = {}, sb[R][V] = {}, w[R][V];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int c = (r * gl + lane) * V;
+        load_columns<V>(a.w, c, count_of<V, WHOLE>(c, a.C), 1.0f, w[r]);
+    }
     for (int64_t q = (int64_t)blockIdx.x * groups + threadIdx.x / gl; q < a.N; q += (int64_t)gridDim.x * groups) {
         const T* x = (const T*)a.x + q * a.x_stride;
         const T* dy = (const T*)a.dy + q * a.dy_stride;
         float xhat[R][V], g[R][V], s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int c = (r * gl + lane) * V;
-            if (c < a.C) {
-                load_pack<V>(x + c, xhat[r]);
-                load_pack<V>(dy + c, g[r]);
+            const int c = (r * gl + lane) * V, n = count_of<V, WHOLE>(c, a.C);
+            const auto px = load_upto<V>(x + c, n), pd = load_upto<V>(dy + c, n);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                xhat[r][i] = to_f32(px.v[i]);
+                g[r][i] = to_f32(pd.v[i]);  // (zero past C: nothing in any sum)
             }
         }
         const float mean = a.mean[q], rstd = a.rstd[q];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int c = (r * gl + lane) * V;
-            if (c < a.C)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    xhat[r][i] = (xhat[r][i] - mean) * rstd;
-                    sw[r][i] += g[r][i] * xhat[r][i];
-                    sb[r][i] += g[r][i];
-                    g[r][i] *= a.w ? a.w[c + i] : 1.0f;
-                    s1 += g[r][i];
-                    s2 += g[r][i] * xhat[r][i];
-                }
-        }
+            for (int i = 0; i < V; ++i) {
+                xhat[r][i] = (xhat[r][i] - mean) * rstd;
+                sw[r][i] += g[r][i] * xhat[r][i];
+                sb[r][i] += g[r][i];
+                g[r][i] *= w[r][i];
+                s1 += g[r][i];
+                s2 += g[r][i] * xhat[r][i];
+            }
         if (!a.out) continue;
-        s1 = sum_within(s1, gl) * per;
-        s2 = sum_within(s2, gl) * per;
+        s1 = sum_within(s1, gl) * per * rstd;
+        s2 = sum_within(s2, gl) * per * rstd;
         T* dx = (T*)a.out + q * a.C;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int c = (r * gl + lane) * V;
-            if (c < a.C) {
+            Pack<T, V> p;
 #pragma unroll
-                for (int i = 0; i < V; ++i) g[r][i] = rstd * (g[r][i] - s1 - xhat[r][i] * s2);
-                store_pack<V>(dx + c, g[r]);
-            }
+            for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(rstd * g[r][i] - s1 - xhat[r][i] * s2);
+            store_upto<V>(dx + c, count_of<V, WHOLE>(c, a.C), p);
         }
     }
     if (!a.part) return;
@@ -140,16 +163,15 @@ __global__ void __launch_bounds__(kThreads) rows_backward(const NormArgs a, int 
 
 // Lanes a row and vectors a lane for n vectors: the fewest idle lanes, of those
 // the most vectors a lane (more bytes on their way, fewer steps of the sums).
-bool layout(int n, int most, int& gl, int& r)
+bool layout(int n, int& gl, int& r)
 {
     int best = 0;
-    for (int t = 1; t <= most; t = t < 4 ? t + 1 : t * 2) {
+    for (int t : {1, 2, 3, 4, 8}) {
         int lanes = 1;
         while (lanes * t < n) lanes *= 2;
-        if (lanes > 64) continue;
+        if (lanes > 64 || (t > 4 && best)) continue;
         const int used = n * 1024 / (lanes * t);
         if (used < best) continue;
-        if (t > 4 && best) break;
         best = used;
         gl = lanes;
         r = t;
@@ -157,34 +179,29 @@ bool layout(int n, int most, int& gl, int& r)
     return best != 0;
 }
 
-template <typename T, int V, int R>
+template <typename T, int R, bool WHOLE>
 void launch_r(bool forward, const NormArgs& a, int gl, hipStream_t s)
 {
     const int groups = kThreads / gl;
     if (forward)
-        hipLaunchKernelGGL((rows_forward<T, V, R>), dim3((unsigned)((a.N + groups - 1) / groups)), dim3(kThreads), 0, s,
-                           a, gl);
+        hipLaunchKernelGGL((rows_forward<T, R, WHOLE>), dim3((unsigned)((a.N + groups - 1) / groups)), dim3(kThreads),
+                           0, s, a, gl);
     else
-        hipLaunchKernelGGL((rows_backward<T, V, R>), dim3(a.nparts), dim3(kThreads), (size_t)a.C * 8, s, a, gl);
+        hipLaunchKernelGGL((rows_backward<T, R, WHOLE>), dim3(a.nparts), dim3(kThreads), (size_t)a.C * 8, s, a, gl);
 }
 
-template <typename T, int V>
+template <typename T, bool WHOLE>
 bool launch_v(bool forward, const NormArgs& a, hipStream_t s)
 {
+    constexpr int V = 16 / sizeof(T);
     int gl = 0, r = 0;
-    if (a.C % V || !layout(a.C / V, V == 1 ? 32 : 16 / sizeof(T) == V ? 8 : 16, gl, r)) return false;
+    if (!layout((a.C + V - 1) / V, gl, r)) return false;
     switch (r) {
-        case 1: launch_r<T, V, 1>(forward, a, gl, s); return true;
-        case 2: launch_r<T, V, 2>(forward, a, gl, s); return true;
-        case 3: launch_r<T, V, 3>(forward, a, gl, s); return true;
-        case 4: launch_r<T, V, 4>(forward, a, gl, s); return true;
-        case 8: launch_r<T, V, 8>(forward, a, gl, s); return true;
-        case 16:
-            if constexpr (V == 1) launch_r<T, V, 16>(forward, a, gl, s);
-            return V == 1;
-        case 32:
-            if constexpr (V == 1) launch_r<T, V, 32>(forward, a, gl, s);
-            return V == 1;
+        case 1: launch_r<T, 1, WHOLE>(forward, a, gl, s); return true;
+        case 2: launch_r<T, 2, WHOLE>(forward, a, gl, s); return true;
+        case 3: launch_r<T, 3, WHOLE>(forward, a, gl, s); return true;
+        case 4: launch_r<T, 4, WHOLE>(forward, a, gl, s); return true;
+        case 8: launch_r<T, 8, WHOLE>(forward, a, gl, s); return true;
     }
     return false;
 }
@@ -192,11 +209,7 @@ bool launch_v(bool forward, const NormArgs& a, hipStream_t s)
 template <typename T>
 bool launch_t(bool forward, const NormArgs& a, hipStream_t s)
 {
-    constexpr int W = 16 / sizeof(T);
-    const uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.out | (uintptr_t)a.dy;
-    if (all % 16 == 0 && a.x_stride % W == 0 && (forward || a.dy_stride % W == 0) && launch_v<T, W>(forward, a, s))
-        return true;
-    return launch_v<T, 1>(forward, a, s);
+    return a.C % (16 / (int)sizeof(T)) == 0 ? launch_v<T, true>(forward, a, s) : launch_v<T, false>(forward, a, s);
 }
 
 bool launch(wtconv_dtype dt, bool forward, const NormArgs& a, hipStream_t s)

@@ -1,6 +1,12 @@
-// Scaled residual between planes and rows, forward and backward.
-#include "block_internal.h"
-#include "wtconv_device.h"
+// Scaled residual between planes and rows, forward and backward: one read of
+// every input, one write of every output. Bound by memory.
+//
+// A workgroup takes tiles of P pixels by a block of channels; rows are turned in
+// LDS (turn.h), where a thread's own units are its own on both ways, so that z
+// comes in and dz goes out through the same place without a barrier between.
+// The backward pass keeps its channels' part of d_gamma in registers over all of
+// its tiles.
+#include "turn.h"
 
 namespace wtc {
 namespace {
@@ -14,9 +20,13 @@ DEV float wave_sum(float v)
     return v;
 }
 
+// ----------------------------------------------------------------------------
+// tensors whose offsets pass 32 bits within a tile
+// ----------------------------------------------------------------------------
+
 // Workgroup: 64 channels (blockIdx.y), one tile of 64 pixels after another.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) residual_forward(const ResidualArgs a)
+__global__ void __launch_bounds__(kThreads) residual_forward_any(const ResidualArgs a)
 {
     __shared__ T turn[kTile][kTile + 1];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c0 = blockIdx.y * kTile;
@@ -41,7 +51,7 @@ __global__ void __launch_bounds__(kThreads) residual_forward(const ResidualArgs 
 
 // dz, and the partial sums for d_gamma of one of nparts runs of tiles (blockIdx.x).
 template <typename T>
-__global__ void __launch_bounds__(kThreads) residual_backward(const ResidualArgs a)
+__global__ void __launch_bounds__(kThreads) residual_backward_any(const ResidualArgs a)
 {
     __shared__ T turn[kTile][kTile + 1], back[kTile][kTile + 1];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c0 = blockIdx.y * kTile;
@@ -83,45 +93,196 @@ __global__ void __launch_bounds__(kThreads) residual_backward(const ResidualArgs
     }
 }
 
-int grid_for(int64_t items, int64_t most) { return (int)(items < most ? (items > 1 ? items : 1) : most); }
+// ----------------------------------------------------------------------------
+// the others
+// ----------------------------------------------------------------------------
 
-template <typename T>
-hipError_t forward_t(const ResidualArgs& a, hipStream_t s)
+DEV float factor(const float* p, int64_t i) { return p ? p[i] : 1.0f; }
+
+// f[g] = scale[c + g], ones without it or past C.
+template <int G>
+DEV void channel_factors(const float* p, int c, int left, float (&f)[G])
 {
-    const dim3 grid(grid_for((a.N + kTile - 1) / kTile, 1 << 16), (a.C + kTile - 1) / kTile);
-    hipLaunchKernelGGL(residual_forward<T>, grid, dim3(kThreads), 0, s, a);
+#pragma unroll
+    for (int g = 0; g < G; ++g) f[g] = p && g < left ? p[c + g] : 1.0f;
+}
+
+template <typename Ti>
+__global__ void __launch_bounds__(Ti::TH) residual_forward(const ResidualArgs a, const Pixels ps)
+{
+    using T = typename Ti::Type;
+    using Tu = Turn<Ti>;
+    constexpr int V = Ti::V, NS = Ti::NS, K = Ti::K, G = Ti::G;
+    static_assert(Tu::kSteps == K, "a block of channels is turned at once");
+    __shared__ uint4 turn[Tu::kSize];
+    const int px = threadIdx.x % Ti::LP, slot = threadIdx.x / Ti::LP, c0 = blockIdx.y * Ti::kMaxC;
+    const Place<Ti> at(ps, blockIdx.x, px, slot);
+    const T* x = (const T*)a.x + c0 * a.S;
+    T* y = (T*)a.out + c0 * a.S;
+    float v[K][V][G];
+    int left[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        left[k] = at.left(a.C - c0, slot, k);
+        load_pixels<Ti>(x, at, a.S, left[k], k, v[k]);
+    }
+    Tu::template copy<false>((const T*)a.z + (int64_t)at.q0 * a.C + c0, a.C, turn, at.rows,
+                             a.C - c0 < Tu::kWidth ? a.C - c0 : Tu::kWidth);
+    const float keep = factor(a.keep, at.image);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (left[k] <= 0) continue;
+        float z[V][G], scale[G];
+        Tu::get(turn, px, k * NS + slot, z);
+        channel_factors<G>(a.gamma, c0 + (k * NS + slot) * G, left[k], scale);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[k][i][g] += scale[g] * keep * z[i][g];
+        store_pixels<Ti>(y, at, a.S, left[k], k, v[k]);
+    }
+}
+
+template <typename Ti>
+__global__ void __launch_bounds__(Ti::TH) residual_backward(const ResidualArgs a, const Pixels ps)
+{
+    using T = typename Ti::Type;
+    using Tu = Turn<Ti>;
+    constexpr int V = Ti::V, NS = Ti::NS, K = Ti::K, G = Ti::G;
+    static_assert(Tu::kSteps == K, "a block of channels is turned at once");
+    __shared__ uint4 turn[Tu::kSize];
+    const int px = threadIdx.x % Ti::LP, slot = threadIdx.x / Ti::LP, c0 = blockIdx.y * Ti::kMaxC;
+    const int width = a.C - c0 < Tu::kWidth ? a.C - c0 : Tu::kWidth;
+    const T* dy = (const T*)a.x + c0 * a.S;
+    float sum[K][G] = {};
+    for (uint32_t tile = blockIdx.x; tile < ps.tiles; tile += gridDim.x) {
+        const Place<Ti> at(ps, tile, px, slot);
+        float d[K][V][G];
+        int left[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            left[k] = at.left(a.C - c0, slot, k);
+            load_pixels<Ti>(dy, at, a.S, left[k], k, d[k]);
+        }
+        const float keep = factor(a.keep, at.image);
+        if (a.part) {
+            Tu::template copy<false>((const T*)a.z + (int64_t)at.q0 * a.C + c0, a.C, turn, at.rows, width);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (left[k] <= 0) continue;
+            float z[V][G], scale[G];
+            if (a.part) Tu::get(turn, px, k * NS + slot, z);
+            channel_factors<G>(a.gamma, c0 + (k * NS + slot) * G, left[k], scale);
+            over_channels<Ti>(left[k], [&](int g) ALWAYS {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    if (a.part) sum[k][g] += d[k][i][g] * z[i][g] * keep;
+                    d[k][i][g] *= scale[g] * keep;
+                }
+            });
+            if (a.out) Tu::put(turn, px, k * NS + slot, d[k]);
+        }
+        __syncthreads();
+        if (a.out) {
+            Tu::template copy<true>((T*)a.out + (int64_t)at.q0 * a.C + c0, a.C, turn, at.rows, width);
+            __syncthreads();
+        }
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int c = c0 + (k * NS + slot) * G + g;
+#pragma unroll
+            for (int o = Ti::LP >> 1; o; o >>= 1) sum[k][g] += __shfl_xor(sum[k][g], o);
+            if (px == 0 && c < a.C) a.part[(int64_t)blockIdx.x * a.C + c] = sum[k][g];
+        }
+}
+
+// Channels of a block: 96 or 128, whichever leaves fewer lanes idle in the last
+// one (96 and its multiples are this kind of network's widths).
+int block_channels(int C) { return (C + 95) / 96 * 96 < (C + 127) / 128 * 128 ? 96 : 128; }
+
+template <typename Ti>
+bool launch(bool forward, const ResidualArgs& a, hipStream_t s)
+{
+    Pixels ps;
+    if (!pixels_of<Ti>(a.B, a.S, a.C, ps)) return false;
+    const unsigned blocks = (unsigned)((a.C + Ti::kMaxC - 1) / Ti::kMaxC);
+    if (forward)
+        hipLaunchKernelGGL(residual_forward<Ti>, dim3(ps.tiles, blocks), dim3(Ti::TH), 0, s, a, ps);
+    else
+        hipLaunchKernelGGL(residual_backward<Ti>, dim3(a.nparts, blocks), dim3(Ti::TH), 0, s, a, ps);
+    return true;
+}
+
+template <typename T, int V, bool REGULAR>
+bool launch_tile(bool forward, const ResidualArgs& a, hipStream_t s)
+{
+    constexpr int E = sizeof(T) / 2;  // 16-byte units of float32 hold half the channels: twice the steps
+    if constexpr (V == 4) {
+        if (block_channels(a.C) == 96) return launch<Tile<T, 192, 4, 16, E, REGULAR>>(forward, a, s);
+        return launch<Tile<T, 256, 4, 16, E, REGULAR>>(forward, a, s);
+    } else {
+        if (block_channels(a.C) == 96) return launch<Tile<T, 192, 1, 64, 4 * E, false>>(forward, a, s);
+        return launch<Tile<T, 256, 1, 64, 4 * E, false>>(forward, a, s);
+    }
+}
+
+// Vectors of four pixels, but for images so small that most tiles of 64 pixels
+// would be empty: single pixels then run over all images.
+template <typename T>
+hipError_t launch_t(bool forward, const ResidualArgs& a, hipStream_t s)
+{
+    bool done;
+    if (a.S % 4 == 0 && a.C % (16 / (int)sizeof(T)) == 0)
+        done = launch_tile<T, 4, true>(forward, a, s);
+    else if (a.S >= 32 && launch_tile<T, 4, false>(forward, a, s))
+        done = true;
+    else
+        done = launch_tile<T, 1, false>(forward, a, s);
+    if (!done) {
+        const unsigned blocks = (unsigned)((a.C + kTile - 1) / kTile);
+        if (forward)
+            hipLaunchKernelGGL(residual_forward_any<T>, dim3(at_most((a.N + kTile - 1) / kTile, 1 << 16), blocks),
+                               dim3(kThreads), 0, s, a);
+        else
+            hipLaunchKernelGGL(residual_backward_any<T>, dim3(a.nparts, blocks), dim3(kThreads), 0, s, a);
+    }
     return hipGetLastError();
 }
 
-template <typename T>
-hipError_t backward_t(const ResidualArgs& a, hipStream_t s)
-{
-    hipLaunchKernelGGL(residual_backward<T>, dim3(a.nparts, (a.C + kTile - 1) / kTile), dim3(kThreads), 0, s, a);
-    return hipGetLastError();
-}
-
-}  // namespace
-
-int64_t residual_parts(const wtconv_residual_desc& d) { return grid_for((d.B * d.S + kTile - 1) / kTile, 512); }
-
-hipError_t launch_residual_forward(wtconv_dtype dt, const ResidualArgs& a, hipStream_t s)
+hipError_t launch_type(wtconv_dtype dt, bool forward, const ResidualArgs& a, hipStream_t s)
 {
     switch (dt) {
-        case WTCONV_F32: return forward_t<float>(a, s);
-        case WTCONV_BF16: return forward_t<uint16_t>(a, s);
-        case WTCONV_F16: return forward_t<_Float16>(a, s);
+        case WTCONV_F32: return launch_t<float>(forward, a, s);
+        case WTCONV_BF16: return launch_t<uint16_t>(forward, a, s);
+        case WTCONV_F16: return launch_t<_Float16>(forward, a, s);
     }
     return hipErrorInvalidValue;
 }
 
+}  // namespace
+
+// Four workgroups a CU over all blocks of channels.
+int64_t residual_parts(const wtconv_residual_desc& d)
+{
+    const int64_t blocks = (d.C + block_channels(d.C) - 1) / block_channels(d.C);
+    return at_most((d.B * d.S + kTile - 1) / kTile, blocks < 16 ? 1024 / blocks : 64);
+}
+
+hipError_t launch_residual_forward(wtconv_dtype dt, const ResidualArgs& a, hipStream_t s)
+{
+    return launch_type(dt, true, a, s);
+}
+
 hipError_t launch_residual_backward(wtconv_dtype dt, ResidualArgs a, float* dgamma, hipStream_t s)
 {
-    hipError_t e = hipErrorInvalidValue;
-    switch (dt) {
-        case WTCONV_F32: e = backward_t<float>(a, s); break;
-        case WTCONV_BF16: e = backward_t<uint16_t>(a, s); break;
-        case WTCONV_F16: e = backward_t<_Float16>(a, s); break;
-    }
+    const hipError_t e = launch_type(dt, false, a, s);
     if (e != hipSuccess || !a.part) return e;
     return launch_sum_parts(a.part, a.nparts, a.C, a.C, dgamma, nullptr, s);
 }

@@ -1,4 +1,4 @@
-// Turning tiles between planes and rows.
+// Tiles of pixels and channels, turned between planes and rows.
 //
 // In planes a thread reads V adjacent pixels of a channel, in rows G = 16 bytes
 // of adjacent channels of a pixel. A thread that holds V pixels of G channels
@@ -14,12 +14,16 @@
 namespace wtc {
 
 // TH threads: LP lanes of V pixels side by side, NS slots of K * G channels.
-// WHOLE: C is a multiple of G.
-template <typename T, int TH_, int V_, int LP_, int K_, bool WHOLE>
+// REGULAR: C is a multiple of G and S one of V, so that no unit and no vector is
+// incomplete.
+template <typename T, int TH_, int V_, int LP_, int K_, bool REGULAR>
 struct Tile {
     using Type = T;
     static constexpr int TH = TH_, V = V_, LP = LP_, K = K_, G = 16 / (int)sizeof(T);
-    static constexpr bool kWhole = WHOLE;
+    static constexpr bool kRegular = REGULAR;
+    // Tiles run over all images' pixels where no vector crosses from one image to
+    // the next, else over each image's by itself.
+    static constexpr bool kFlat = REGULAR || V == 1;
     static constexpr int P = LP * V, NS = TH / LP, NW = TH / 64;
     static constexpr int kChannels = NS * G;       // channels of one step k
     static constexpr int kMaxC = kChannels * K;
@@ -42,13 +46,21 @@ constexpr int turn_steps()
     return n;
 }
 
+// i / per for i * per < 2^32, per > 0
+struct Divider {
+    int per;
+    uint32_t magic;
+    DEV explicit Divider(int n) : per(n), magic(0xffffffffu / (uint32_t)n + 1u) {}
+    DEV int operator()(int i) const { return per == 1 ? i : (int)__umulhi((uint32_t)i, magic); }
+};
+
 template <typename Ti>
 struct Turn {
     using T = typename Ti::Type;
+    using Unit = Pack<T, Ti::G>;
     static constexpr int kSteps = turn_steps<Ti>(), U = turn_units<Ti>(kSteps), kWidth = kSteps * Ti::kChannels;
     static constexpr int kSize = Ti::P * U;
 
-    static DEV int at(int p, int u) { return p * U + turned(p / Ti::V, u); }
     // The place of unit u in every pixel of lane px.
     static DEV int turned(int px, int u)
     {
@@ -63,7 +75,7 @@ struct Turn {
         uint4* first = lds + px * Ti::V * U + turned(px, u);
 #pragma unroll
         for (int i = 0; i < Ti::V; ++i) {
-            Pack<T, Ti::G> q;
+            Unit q;
 #pragma unroll
             for (int g = 0; g < Ti::G; ++g) q.v[g] = from_f32<T>(f[i][g]);
             first[i * U] = __builtin_bit_cast(uint4, q);
@@ -74,141 +86,133 @@ struct Turn {
         const uint4* first = lds + px * Ti::V * U + turned(px, u);
 #pragma unroll
         for (int i = 0; i < Ti::V; ++i) {
-            const auto q = __builtin_bit_cast(Pack<T, Ti::G>, first[i * U]);
+            const auto q = __builtin_bit_cast(Unit, first[i * U]);
 #pragma unroll
             for (int g = 0; g < Ti::G; ++g) f[i][g] = to_f32(q.v[g]);
         }
     }
 
     // The rows' side: `rows` rows of `width` channels, `pitch` elements apart, to
-    // or from memory. Whole units where they are aligned; else elements, two at
-    // once where 16-bit rows follow each other without a gap.
+    // or from memory. What comes in is followed by rows of zeros up to P.
     template <bool OUT>
     static DEV void copy(std::conditional_t<OUT, T, const T>* mem, int64_t pitch, uint4* lds, int rows, int width)
     {
-        if (width % Ti::G == 0 && pitch % Ti::G == 0 && (uintptr_t)mem % 16 == 0) {
-            using M = std::conditional_t<OUT, uint4, const uint4>;
-            const int per = width / Ti::G, n = rows * per;
-            const uint32_t magic = divider(per);
-            const int dr = divide(Ti::TH, per, magic), du = Ti::TH - dr * per;
-            int r = divide(threadIdx.x, per, magic), u = threadIdx.x - r * per;
-            const bool dense = pitch == width;
+        const int per = (width + Ti::G - 1) / Ti::G, n = rows * per, tail = width - (per - 1) * Ti::G;
+        const Divider over(per);
+        const int dr = over(Ti::TH), du = Ti::TH - dr * per;
+        int r = over(threadIdx.x), u = threadIdx.x - r * per;
+        const bool dense = Ti::kRegular && pitch == width;
 #pragma unroll 4
-            for (int i = threadIdx.x; i < n; i += Ti::TH) {
-                M* m = dense ? reinterpret_cast<M*>(mem) + i : reinterpret_cast<M*>(mem + r * pitch) + u;
-                if constexpr (OUT)
-                    *m = lds[at(r, u)];
-                else
-                    lds[at(r, u)] = *m;
-                r += dr;
-                u += du;
-                if (u >= per) {
-                    u -= per;
-                    ++r;
-                }
-            }
-            return;
-        }
-        T* elements = reinterpret_cast<T*>(lds);
-        auto element = [&](int r, int c) -> T& { return elements[at(r, c / Ti::G) * Ti::G + c % Ti::G]; };
-        const uint32_t magic = divider(width);
-        const int n = rows * width;
-        if (sizeof(T) == 2 && (pitch == width || rows == 1) && (uintptr_t)mem % 4 == 0) {
-            for (int i = threadIdx.x * 2; i < n; i += Ti::TH * 2) {
-                const int r = divide(i, width, magic), c = i - r * width;
-                const bool last = i + 1 == n;
-                const int r2 = c + 1 == width ? r + 1 : r, c2 = c + 1 == width ? 0 : c + 1;
-                if constexpr (OUT) {
-                    const T v = element(r, c);
-                    if (last)
-                        mem[i] = v;
-                    else
-                        *reinterpret_cast<Pack<T, 2>*>(mem + i) = {{v, element(r2, c2)}};
-                } else if (last) {
-                    element(r, c) = mem[i];
-                } else {
-                    const auto q = *reinterpret_cast<const Pack<T, 2>*>(mem + i);
-                    element(r, c) = q.v[0];
-                    element(r2, c2) = q.v[1];
-                }
-            }
-            return;
-        }
         for (int i = threadIdx.x; i < n; i += Ti::TH) {
-            const int r = divide(i, width, magic), c = i - r * width;
+            auto* m = dense ? mem + i * Ti::G : mem + r * pitch + u * Ti::G;
+            uint4* t = lds + r * U + turned(r / Ti::V, u);
+            const int count = Ti::kRegular || u + 1 < per ? Ti::G : tail;
             if constexpr (OUT)
-                mem[r * pitch + c] = element(r, c);
+                store_upto<Ti::G>(m, count, __builtin_bit_cast(Unit, *t));
             else
-                element(r, c) = mem[r * pitch + c];
+                *t = __builtin_bit_cast(uint4, load_upto<Ti::G>(m, count));
+            r += dr;
+            u += du;
+            if (u >= per) {
+                u -= per;
+                ++r;
+            }
         }
+        if (!OUT && rows < Ti::P)
+            for (int i = rows * U + threadIdx.x; i < Ti::P * U; i += Ti::TH) lds[i] = uint4{0, 0, 0, 0};
     }
-
-    // i / per for i * per < 2^32, per > 0
-    static DEV uint32_t divider(int per) { return 0xffffffffu / (uint32_t)per + 1u; }
-    static DEV int divide(int i, int per, uint32_t magic) { return per == 1 ? i : (int)__umulhi((uint32_t)i, magic); }
 };
 
-// Where a thread's pixels and channels lie in planes: bytes from the first
-// image of its tile on, as 32 bits from an address that is the same for the
-// whole workgroup (the host checks that they suffice), so that the loads of all
-// channels share one register of addresses.
+// The planes that tiles run over, and n / d for n < 2^31 as (n * magic) >> shift.
 struct Pixels {
     int64_t S;       // pixels of an image
-    uint64_t magic;  // ceil(2^shift / S): q / S for q < 2^31
+    uint64_t magic;  // of S in flat tiles, of an image's tiles in others
     int shift;
     int C;
+    uint32_t N;      // pixels of all images
+    uint32_t tiles, per_image;
 
-    DEV uint32_t image(uint32_t q) const { return (uint32_t)((q * magic) >> shift); }
+    DEV uint32_t quotient(uint32_t n) const { return (uint32_t)((n * magic) >> shift); }
 };
 
+// The tiles of B images of S pixels; false where 32 bits do not hold the bytes
+// of a tile from its first image on, or the pixels' numbers.
 template <typename Ti>
-bool pixels_fit(int64_t N, int64_t S, int C)
+bool pixels_of(int64_t B, int64_t S, int C, Pixels& p)
 {
-    return N < (int64_t)1 << 31 && ((int64_t)Ti::P + 2 * S) * C + (int64_t)Ti::kChannels * S <
-                                       ((int64_t)1 << 32) / (int64_t)sizeof(typename Ti::Type);
-}
-
-inline Pixels pixels_of(int64_t S, int C)
-{
-    Pixels p;
+    const int64_t N = B * S, e = sizeof(typename Ti::Type), bytes = (int64_t)1 << 32;
+    if (N < 1 || N >= (int64_t)1 << 31) return false;
+    if (((Ti::kFlat ? (Ti::P + 2 * S) * C : Ti::P) + (int64_t)Ti::kChannels * S) * e >= bytes) return false;
     p.S = S;
     p.C = C;
+    p.N = (uint32_t)N;
+    p.per_image = (uint32_t)((S + Ti::P - 1) / Ti::P);
+    p.tiles = Ti::kFlat ? (uint32_t)((N + Ti::P - 1) / Ti::P) : (uint32_t)B * p.per_image;
+    const int64_t d = Ti::kFlat ? S : p.per_image;
     p.shift = 31;
-    while (((int64_t)1 << (p.shift - 31)) < S && p.shift < 62) ++p.shift;
-    p.magic = S > 0 ? (((uint64_t)1 << p.shift) + S - 1) / S : 0;
-    return p;
+    while (((int64_t)1 << (p.shift - 31)) < d) ++p.shift;
+    p.magic = (((uint64_t)1 << p.shift) + d - 1) / d;
+    return true;
 }
 
+// Where a tile and a thread's pixels and channels lie. Planes are addressed by
+// bytes from an element that is the same for the whole workgroup, so that the
+// loads of all channels share one register of addresses.
 template <typename Ti>
 struct Place {
-    int64_t base;   // first element of the tile's first image, the same for all threads
-    uint32_t bytes; // from there to channel slot * G of this thread's first pixel
+    using T = typename Ti::Type;
+    uint32_t q0;    // the tile's first pixel, and its number of pixels
+    int rows;
+    uint32_t q;     // the thread's first pixel, and its number of pixels, up to V
+    int count;
+    uint32_t image; // of the thread's pixels
+    int64_t base;   // element of the planes
+    uint32_t bytes; // from there to channel slot * G of the thread's first pixel
 
-    DEV Place(const Pixels& p, uint32_t q0, uint32_t q, int slot)
+    DEV Place(const Pixels& p, uint32_t tile, int px, int slot)
     {
-        using T = typename Ti::Type;
-        const uint32_t b0 = p.image(q0), b = p.image(q);
-        base = (int64_t)b0 * p.C * p.S;
-        bytes = ((b - b0) * (uint32_t)p.C * (uint32_t)p.S + (q - b * (uint32_t)p.S) +
-                 (uint32_t)slot * Ti::G * (uint32_t)p.S) * (uint32_t)sizeof(T);
+        const uint32_t S = (uint32_t)p.S;
+        if constexpr (Ti::kFlat) {
+            q0 = tile * Ti::P;
+            q = q0 + px * Ti::V;
+            rows = p.N - q0 < Ti::P ? (int)(p.N - q0) : Ti::P;
+            count = q < p.N ? Ti::V : 0;
+            const uint32_t b0 = p.quotient(q0);
+            image = count ? p.quotient(q) : b0;
+            base = (int64_t)b0 * p.C * p.S;
+            bytes = count ? (image - b0) * (uint32_t)p.C * S + (q - image * S) : 0;
+        } else {
+            image = p.quotient(tile);
+            const uint32_t s0 = (tile - image * p.per_image) * Ti::P;
+            q0 = image * S + s0;
+            q = q0 + px * Ti::V;
+            rows = S - s0 < Ti::P ? (int)(S - s0) : Ti::P;
+            const int n = rows - px * Ti::V;
+            count = n < 0 ? 0 : n < Ti::V ? n : Ti::V;
+            base = (int64_t)image * p.C * p.S + s0;
+            bytes = px * Ti::V;
+        }
+        bytes = (bytes + (uint32_t)(slot * Ti::G) * S) * (uint32_t)sizeof(T);
     }
+    // Channels of the thread's unit of step k that there are, of C; more than G
+    // where others follow, none or less where there is no unit.
+    DEV int left(int C, int slot, int k) const { return count ? C - (k * Ti::NS + slot) * Ti::G : 0; }
+
     // The thread's pixels in channel (k * NS + slot) * G + g.
-    template <typename U>
-    DEV U* at(U* p, int64_t S, int k, int g) const
+    template <typename E>
+    DEV E* at(E* p, int64_t S, int k, int g) const
     {
-        using B = std::conditional_t<std::is_const_v<U>, const char, char>;
+        using B = std::conditional_t<std::is_const_v<E>, const char, char>;
         B* first = reinterpret_cast<B*>(p + base + (k * Ti::kChannels + g) * S);
-        return reinterpret_cast<U*>(first + bytes);
+        return reinterpret_cast<E*>(first + bytes);
     }
 };
 
-// Calls f(g) for each of the thread's channels of a step that there are, `left`
-// of them from its first on. Where C is a multiple of G a unit is whole or not
-// there, and one test is enough.
+// Calls f(g) for each channel of a thread's unit that there is.
 template <typename Ti, typename F>
 DEV void over_channels(int left, F&& f)
 {
-    if constexpr (Ti::kWhole) {
+    if constexpr (Ti::kRegular) {
         if (left > 0) {
 #pragma unroll
             for (int g = 0; g < Ti::G; ++g) f(g);
@@ -220,27 +224,26 @@ DEV void over_channels(int left, F&& f)
     }
 }
 
-// The thread's V pixels of its G channels of step k; what is past C is not
-// written.
+// The thread's pixels of its unit of step k; zeros for pixels that are not
+// there, nothing for channels.
 template <typename Ti, typename T = typename Ti::Type>
-DEV void load_pixels(const T* p, const Place<Ti>& at, const Pixels& px, int left, int k, float (&f)[Ti::V][Ti::G])
+DEV void load_pixels(const T* p, const Place<Ti>& at, int64_t S, int left, int k, float (&f)[Ti::V][Ti::G])
 {
     over_channels<Ti>(left, [&](int g) ALWAYS {
-        float v[Ti::V];
-        load_pack<Ti::V>(at.at(p, px.S, k, g), v);
+        const auto q = load_upto<Ti::V>(at.at(p, S, k, g), Ti::kFlat ? Ti::V : at.count);
 #pragma unroll
-        for (int i = 0; i < Ti::V; ++i) f[i][g] = v[i];
+        for (int i = 0; i < Ti::V; ++i) f[i][g] = to_f32(q.v[i]);
     });
 }
 
 template <typename Ti, typename T = typename Ti::Type>
-DEV void store_pixels(T* p, const Place<Ti>& at, const Pixels& px, int left, int k, const float (&f)[Ti::V][Ti::G])
+DEV void store_pixels(T* p, const Place<Ti>& at, int64_t S, int left, int k, const float (&f)[Ti::V][Ti::G])
 {
     over_channels<Ti>(left, [&](int g) ALWAYS {
-        float v[Ti::V];
+        Pack<T, Ti::V> q;
 #pragma unroll
-        for (int i = 0; i < Ti::V; ++i) v[i] = f[i][g];
-        store_pack<Ti::V>(at.at(p, px.S, k, g), v);
+        for (int i = 0; i < Ti::V; ++i) q.v[i] = from_f32<T>(f[i][g]);
+        store_upto<Ti::V>(at.at(p, S, k, g), Ti::kFlat ? Ti::V : at.count, q);
     });
 }
 
