@@ -352,7 +352,8 @@ wtconv_status wtconv_scaled_residual_backward(const wtconv_residual_desc* desc, 
  * from its `offset` on, a multiple of 64 elements; a buffer holds the last
  * tensor's elements rounded up to 64. state_bits = 32: float32. state_bits = 8:
  * one byte for each element, and one scale byte for each 64 elements, in two
- * buffers more. The scale is the biased exponent of the largest magnitude of
+ * buffers more; the rest of a tensor's last 64 bytes is zero before its first
+ * step and stays so. The scale is the biased exponent of the largest magnitude of
  * its block, 255 if one is not finite (the block then stands for NaN). A code
  * of m is a sign, 4 bits of exponent and 3 of mantissa, one of v 5 bits of
  * exponent and 3 of mantissa: the float32 with these bits below its sign

@@ -1,12 +1,18 @@
-// AdamW over many tensors, with moments in 32 or 8 bits.
-#include "block_internal.h"
-#include "wtconv_device.h"
+// AdamW over many tensors, with moments in 32 or 8 bits: one read and one write
+// of every parameter and moment, one read of every gradient.
+//
+// A workgroup takes one chunk of one tensor; which, its wavefronts find among
+// the launch's tensors with one load and a vote. Bound by memory with 32-bit
+// moments (28 bytes an element in float32); with 8-bit moments (16.06 bytes) the
+// arithmetic of the codes takes about half of the time that memory does and runs
+// under it.
+#include "norm_device.h"
 
 namespace wtc {
 namespace {
 
 constexpr int kThreads = 256, kVec = 4;
-constexpr int kChunk = 8 * kThreads * kVec;  // elements of one workgroup
+constexpr int kChunk = 2 * kThreads * kVec;  // elements of one workgroup
 constexpr int kMTop = 14, kVTop = 30;        // exponent field of a block's largest moment
 
 // 32 random bits for an element's place under a key.
@@ -18,137 +24,141 @@ DEV uint32_t random_bits(uint32_t place, uint32_t key)
     return x ^ (x >> 16);
 }
 
-// The largest of the 16 lanes that hold a block of 64 elements.
-DEV uint32_t block_max(uint32_t v)
+// The values that four codes stand for under their block's scale: the float that
+// has a code's exponent and mantissa bits below its sign, times 2^(scale - top);
+// NaN under scale 255.
+template <bool SIGNED>
+DEV void decode(uint32_t codes, int scale, float (&f)[kVec])
 {
+    const uint32_t nan = scale == 255 ? 0x7fc00000u : 0u;
 #pragma unroll
-    for (int o = 8; o; o >>= 1) {
-        const uint32_t u = __shfl_xor(v, o);
-        v = u > v ? u : v;
-    }
-    return v;
-}
-
-// The value that a code's low bits stand for under its block's scale.
-DEV float decode(uint32_t code, int scale, int top)
-{
-    const float v = __builtin_ldexpf(__uint_as_float(code << 20), scale - top);
-    return scale == 255 ? __uint_as_float(0x7fc00000u) : v;
-}
-
-// The code's low bits of a magnitude under its block's scale.
-DEV uint32_t encode(float mag, int scale, int top, uint32_t rest)
-{
-    return (__float_as_uint(__builtin_ldexpf(mag, top - scale)) + rest) >> 20;
-}
-
-template <typename T>
-DEV void load_vec(const T* p, int64_t left, bool whole, float (&v)[kVec])
-{
-    if (whole) {
-        struct alignas(sizeof(T) * kVec) Pack { T v[kVec]; };
-        const Pack q = *reinterpret_cast<const Pack*>(p);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = to_f32(q.v[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = i < left ? to_f32(p[i]) : 0.f;
+    for (int i = 0; i < kVec; ++i) {
+        // (a signed code is extended to all bits above it and loses what lies between)
+        const uint32_t bits = SIGNED ? ((uint32_t)(int8_t)(codes >> (8 * i)) << 20 & 0x87f00000u) | nan
+                                     : ((codes >> (8 * i)) & 0xffu) << 20 | nan;
+        f[i] = __builtin_ldexpf(__uint_as_float(bits), scale - (SIGNED ? kMTop : kVTop));
     }
 }
 
-template <typename T>
-DEV void store_vec(T* p, int64_t left, bool whole, const float (&v)[kVec])
+// The codes of four values under their block's scale: 20 mantissa bits are
+// dropped after `rest` was added to them. Zero under scale 255.
+template <bool SIGNED>
+DEV uint32_t encode(const float (&f)[kVec], int scale, const uint32_t (&rest)[kVec])
 {
-    if (whole) {
-        struct alignas(sizeof(T) * kVec) Pack { T v[kVec]; } q;
+    uint32_t c[kVec];
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) q.v[i] = from_f32<T>(v[i]);
-        *reinterpret_cast<Pack*>(p) = q;
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (i < left) p[i] = from_f32<T>(v[i]);
+    for (int i = 0; i < kVec; ++i) {
+        c[i] = (__float_as_uint(__builtin_ldexpf(f[i], (SIGNED ? kMTop : kVTop) - scale)) + rest[i]) >> 20;
+        if (SIGNED) c[i] |= c[i] >> 4 & 0x80u;  // the sign, 11 bits up
     }
+    // the lowest bytes
+    const uint32_t low = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u), high = __builtin_amdgcn_perm(c[3], c[2], 0x04000c0cu);
+    return scale == 255 ? 0u : low | high;
+}
+
+// The biased exponent of the largest magnitude of the 16 lanes' (64 values'), 255
+// if one is not finite.
+template <bool SIGNED>
+DEV int block_scale(const float (&f)[kVec])
+{
+    uint32_t v = 0;
+    const auto larger = [&v](uint32_t u) ALWAYS { v = u > v ? u : v; };
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) larger(__float_as_uint(f[i]) & (SIGNED ? 0x7fffffffu : 0xffffffffu));
+    larger(__float_as_uint(from_lane<0x128>(__uint_as_float(v))));
+    larger(__float_as_uint(from_lane<0x124>(__uint_as_float(v))));
+    larger(__float_as_uint(from_lane<0x122>(__uint_as_float(v))));
+    larger(__float_as_uint(from_lane<0x121>(__uint_as_float(v))));
+    return (int)(v >> 23 & 0xffu);  // (a NaN's sign is no part of it)
+}
+
+// The tensor that this workgroup's chunk is of.
+DEV int find_tensor(const AdamArgs& a)
+{
+    const int lane = threadIdx.x & 63;
+    int t = -1;
+#pragma unroll
+    for (int i = 0; i < (kAdamTensors + 63) / 64; ++i) {
+        const int j = i * 64 + lane;
+        t += __popcll(__ballot(j < a.count && a.first[j < kAdamTensors ? j : 0] <= blockIdx.x));
+    }
+    return __builtin_amdgcn_readfirstlane(t);
+}
+
+// An address for every lane as bytes from one for the workgroup.
+template <typename E>
+DEV E* at_bytes(E* p, uint32_t bytes)
+{
+    using B = std::conditional_t<std::is_const_v<E>, const char, char>;
+    return reinterpret_cast<E*>(reinterpret_cast<B*>(p) + bytes);
 }
 
 template <typename T, bool CODED>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamArgs a)
 {
-    int t = 0;
-    for (int lo = 1, hi = a.count; lo < hi;) {  // the last tensor whose first chunk is not after this one
-        const int mid = (lo + hi) >> 1;
-        if (a.first[mid] <= blockIdx.x) {
-            t = mid;
-            lo = mid + 1;
-        } else {
-            hi = mid;
-        }
-    }
+    const int t = find_tensor(a);
     const AdamGroup& h = a.group[a.of[t]];
-    const int64_t n = a.n[t], e0 = (int64_t)(blockIdx.x - a.first[t]) * kChunk;
-    T* p = (T*)a.p[t];
-    const T* g = (const T*)a.g[t];
+    const int64_t n = a.n[t], e0 = (int64_t)(blockIdx.x - a.first[t]) * kChunk, at0 = a.at[t] + e0;
+    T* p = (T*)a.p[t] + e0;
+    const T* g = (const T*)a.g[t] + e0;
+    using M = std::conditional_t<CODED, uint8_t, float>;
+    M *hm = (M*)h.m + at0, *hv = (M*)h.v + at0;
+    uint8_t *hms = h.ms + (at0 >> 6), *hvs = h.vs + (at0 >> 6);
     const float gscale = a.scale ? *a.scale : 1.0f;
-    const bool aligned = ((uintptr_t)p | (uintptr_t)g) % (sizeof(T) * kVec) == 0;
-    for (int64_t e = e0 + threadIdx.x * kVec; e < e0 + kChunk && (e & ~(int64_t)63) < n; e += kThreads * kVec) {
-        const int64_t left = n - e, at = a.at[t] + e;
-        const bool whole = aligned && left >= kVec;
-        float pv[kVec], gv[kVec], m[kVec], v[kVec];
-        load_vec(p + e, left, whole, pv);
-        load_vec(g + e, left, whole, gv);
-        if (CODED) {
-            const uint32_t mc = *(const uint32_t*)((const uint8_t*)h.m + at);
-            const uint32_t vc = *(const uint32_t*)((const uint8_t*)h.v + at);
-            const int ms = h.ms[at >> 6], vs = h.vs[at >> 6];
+    const uint32_t key = h.key + (uint32_t)((uint64_t)at0 >> 32) * 0x9E3779B1u;  // (a chunk does not cross 2^32: both are multiples of 64)
+    const int end = n - e0 < kChunk ? (int)(n - e0) : kChunk;
+    // (lanes of one block of 64 elements go on or stop together; past a tensor's
+    // end its last block has zeros, which stay zeros)
+    const uint32_t stop = CODED ? (end + 63) & ~63 : end;
+    for (uint32_t c = threadIdx.x * kVec; c < stop; c += kThreads * kVec) {
+        const int left = end - (int)c;
+        auto pp = load_upto<kVec>(at_bytes(p, c * sizeof(T)), left);
+        const auto pg = load_upto<kVec>(at_bytes(g, c * sizeof(T)), left);
+        float m[kVec], v[kVec];
+        if constexpr (CODED) {
+            const uint32_t mc = *(const uint32_t*)at_bytes(hm, c), vc = *(const uint32_t*)at_bytes(hv, c);
+            decode<true>(mc, *at_bytes(hms, c >> 6), m);
+            decode<false>(vc, *at_bytes(hvs, c >> 6), v);
+        } else {
+            const auto pm = load_upto<kVec>(at_bytes(hm, c * 4), left), pv = load_upto<kVec>(at_bytes(hv, c * 4), left);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const uint32_t c = (mc >> (8 * i)) & 0xff;
-                const float d = decode(c & 0x7f, ms, kMTop);
-                m[i] = i < left ? (c & 0x80 ? -d : d) : 0.f;
-                v[i] = i < left ? decode((vc >> (8 * i)) & 0xff, vs, kVTop) : 0.f;
+                m[i] = pm.v[i];
+                v[i] = pv.v[i];
             }
-        } else {
-            load_vec((const float*)h.m + at, left, left >= kVec, m);
-            load_vec((const float*)h.v + at, left, left >= kVec, v);
         }
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            // each product and sum rounded by itself, so that a moment's rounding to a code is reproducible
+            const float gr = to_f32(pg.v[i]) * gscale;
+            {
+                // each product and sum rounded by itself, so that a moment's rounding to a code is reproducible
 #pragma clang fp contract(off)
-            const float gr = gv[i] * gscale;
-            m[i] = m[i] * h.b1 + gr * h.omb1;
-            v[i] = v[i] * h.b2 + gr * gr * h.omb2;
-            pv[i] = pv[i] * h.keep - m[i] / (sqrtf(v[i]) * h.rcorr2 + h.eps) * h.rate;
+                m[i] = m[i] * h.b1 + gr * h.omb1;
+                v[i] = v[i] * h.b2 + gr * gr * h.omb2;
+            }
+            // square root and reciprocal to one unit in the last place: the update is far below the parameter
+            const float denom = __builtin_amdgcn_sqrtf(v[i]) * h.rcorr2 + h.eps;
+            pp.v[i] = from_f32<T>(to_f32(pp.v[i]) * h.keep - m[i] * __builtin_amdgcn_rcpf(denom) * h.rate);
         }
-        store_vec(p + e, left, whole, pv);
-        if (CODED) {
-            uint32_t bm = 0, bv = 0;
+        store_upto<kVec>(at_bytes(p, c * sizeof(T)), left, pp);
+        if constexpr (CODED) {
+            const int ms = block_scale<true>(m), vs = block_scale<false>(v);
+            uint32_t rm[kVec], rv[kVec];
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const uint32_t um = __float_as_uint(m[i]) & 0x7fffffffu, uv = __float_as_uint(v[i]) & 0x7fffffffu;
-                bm = um > bm ? um : bm;
-                bv = uv > bv ? uv : bv;
+                const uint32_t r = random_bits((uint32_t)at0 + c + i, key);
+                rm[i] = (r << 4 & 0xffff0u) | 8;
+                rv[i] = (r >> 12 & 0xffff0u) | 8;
             }
-            const int ms = block_max(bm) >> 23, vs = block_max(bv) >> 23;
-            uint32_t mc = 0, vc = 0;
-            const uint32_t key = h.key + (uint32_t)((uint64_t)at >> 32) * 0x9E3779B1u;
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                const uint32_t r = random_bits((uint32_t)at + i, key);
-                uint32_t c = encode(fabsf(m[i]), ms, kMTop, (r & 0xffffu) << 4 | 8) | (__float_as_uint(m[i]) >> 31) << 7;
-                mc |= (ms == 255 ? 0 : c) << (8 * i);
-                c = encode(v[i], vs, kVTop, (r >> 16) << 4 | 8);
-                vc |= (vs == 255 ? 0 : c) << (8 * i);
-            }
-            *(uint32_t*)((uint8_t*)h.m + at) = mc;
-            *(uint32_t*)((uint8_t*)h.v + at) = vc;
+            *(uint32_t*)at_bytes(hm, c) = encode<true>(m, ms, rm);
+            *(uint32_t*)at_bytes(hv, c) = encode<false>(v, vs, rv);
             if ((threadIdx.x & 15) == 0) {
-                h.ms[at >> 6] = (uint8_t)ms;
-                h.vs[at >> 6] = (uint8_t)vs;
+                *at_bytes(hms, c >> 6) = (uint8_t)ms;
+                *at_bytes(hvs, c >> 6) = (uint8_t)vs;
             }
         } else {
-            store_vec((float*)h.m + at, left, left >= kVec, m);
-            store_vec((float*)h.v + at, left, left >= kVec, v);
+            store_upto<kVec>(at_bytes(hm, c * 4), left, Pack<float, kVec>{{m[0], m[1], m[2], m[3]}});
+            store_upto<kVec>(at_bytes(hv, c * 4), left, Pack<float, kVec>{{v[0], v[1], v[2], v[3]}});
         }
     }
 }
@@ -159,18 +169,17 @@ moments_kernel(int64_t n, const uint8_t* m, const uint8_t* ms, const uint8_t* v,
 {
     for (int64_t e = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kVec; e < n;
          e += (int64_t)gridDim.x * kThreads * kVec) {
-        const uint32_t mc = *(const uint32_t*)(m + e), vc = *(const uint32_t*)(v + e);
-        const int sm = ms[e >> 6], sv = vs[e >> 6];
         float dm[kVec], dv[kVec];
+        decode<true>(*(const uint32_t*)(m + e), ms[e >> 6], dm);
+        decode<false>(*(const uint32_t*)(v + e), vs[e >> 6], dv);
+        Pack<T, kVec> pm, pv;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const uint32_t c = (mc >> (8 * i)) & 0xff;
-            const float d = decode(c & 0x7f, sm, kMTop);
-            dm[i] = c & 0x80 ? -d : d;
-            dv[i] = decode((vc >> (8 * i)) & 0xff, sv, kVTop);
+            pm.v[i] = from_f32<T>(dm[i]);
+            pv.v[i] = from_f32<T>(dv[i]);
         }
-        store_vec(om + e, kVec, true, dm);
-        store_vec(ov + e, kVec, true, dv);
+        store_pack<kVec>(om + e, pm);
+        store_pack<kVec>(ov + e, pv);
     }
 }
 

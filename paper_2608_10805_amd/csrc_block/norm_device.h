@@ -6,6 +6,8 @@
 
 namespace wtc {
 
+#define ALWAYS __attribute__((always_inline))  // (of lambdas: what they capture stays in registers)
+
 // V elements. In memory they need no more than an element's alignment: the
 // copies below become whole vector loads and stores, which the hardware takes
 // from any address.

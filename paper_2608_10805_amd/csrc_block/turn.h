@@ -30,8 +30,6 @@ struct Tile {
     static_assert(NW * 64 == TH && NS * LP == TH && (LP & (LP - 1)) == 0 && (V & (V - 1)) == 0, "whole wavefronts");
 };
 
-#define ALWAYS __attribute__((always_inline))  // (of lambdas: their arrays stay in registers)
-
 constexpr int kTurnBytes = 32 * 1024;  // LDS for it: leaves room for four workgroups a CU and more
 
 template <typename Ti>
