@@ -124,7 +124,7 @@ def load_block(x):
                       for n in ("wtconv_layer_norm_forward", "wtconv_layer_norm_backward_workspace_bytes",
                                 "wtconv_layer_norm_backward", "wtconv_scaled_residual_forward",
                                 "wtconv_scaled_residual_backward_workspace_bytes", "wtconv_scaled_residual_backward",
-                                "wtconv_adamw_step")], _norm_backward, _residual_backward)
+                                "wtconv_adamw_step", "wtconv_adamw_moments")], _norm_backward, _residual_backward)
             _block = ext
     return _block
 

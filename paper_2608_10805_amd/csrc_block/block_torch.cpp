@@ -14,8 +14,10 @@
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/saved_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
 
@@ -24,7 +26,8 @@
 namespace {
 
 using at::Tensor;
-using torch::autograd::AutogradContext;
+using torch::autograd::Node;
+using torch::autograd::SavedVariable;
 using torch::autograd::variable_list;
 using OptTensor = std::optional<Tensor>;
 
@@ -35,6 +38,7 @@ decltype(&wtconv_scaled_residual_forward) residual_forward = nullptr;
 decltype(&wtconv_scaled_residual_backward_workspace_bytes) residual_bytes = nullptr;
 decltype(&wtconv_scaled_residual_backward) residual_backward = nullptr;
 decltype(&wtconv_adamw_step) adamw_fn = nullptr;
+decltype(&wtconv_adamw_moments) moments_fn = nullptr;
 PyObject* python_norm = nullptr;      // autograd._norm_backward
 PyObject* python_residual = nullptr;  // autograd._residual_backward
 PyTypeObject* parameter_type = nullptr;
@@ -44,14 +48,14 @@ struct Refused {
 
 // A strided GPU tensor without wrappers (functorch, subclasses with a dispatch
 // of their own) and without a forward-mode tangent.
-bool plain(const Tensor& t, c10::Device dev)
+bool plain(const Tensor& t, c10::Device dev, bool tangents = true)
 {
     static const c10::DispatchKeySet wrapped(
         {c10::DispatchKey::Python, c10::DispatchKey::PythonTLSSnapshot, c10::DispatchKey::FuncTorchBatched,
          c10::DispatchKey::FuncTorchGradWrapper, c10::DispatchKey::Functionalize, c10::DispatchKey::Conjugate,
          c10::DispatchKey::Negative, c10::DispatchKey::ZeroTensor});
     return t.defined() && t.is_cuda() && t.device() == dev && t.layout() == at::kStrided &&
-           !t.key_set().has_any(wrapped) && !t._fw_grad(0).defined();
+           !t.key_set().has_any(wrapped) && !(tangents && t._fw_grad(0).defined());
 }
 
 bool vector_of(const OptTensor& t, c10::Device dev, int64_t n)
@@ -201,67 +205,82 @@ Tensor norm(const Tensor& x, const OptTensor& w, const OptTensor& b, const NormA
     return y;
 }
 
-struct NormFn : public torch::autograd::Function<NormFn> {
-    static Tensor forward(AutogradContext* ctx, const Tensor& x, const OptTensor& w, const OptTensor& b, double eps,
-                          int64_t in, int64_t out)
+// The saved tensors' and edges' own class rather than torch::autograd::Function:
+// no list of arguments is taken apart and nothing is kept by name.
+struct NormNode : public Node {
+    SavedVariable x_, stats_, w_;
+    NormArguments args;
+    bool has_w = false, released = false;
+
+    std::string name() const override { return "WTConvLayerNorm"; }
+    void release_variables() override
     {
-        Tensor stats;
-        Tensor y = norm(x, w, b, {eps, in, out}, &stats);
-        ctx->save_for_backward({x, stats, w ? *w : Tensor()});
-        ctx->saved_data["eps"] = eps;
-        ctx->saved_data["in"] = in;
-        ctx->saved_data["out"] = out;
-        ctx->saved_data["bias"] = (bool)b;
-        return y;
+        std::lock_guard<std::mutex> lock(mutex_);
+        x_.reset_data();
+        stats_.reset_data();
+        w_.reset_data();
+        released = true;
     }
 
-    static variable_list backward(AutogradContext* ctx, variable_list grads)
+    variable_list apply(variable_list&& grads) override
     {
-        const variable_list saved = ctx->get_saved_variables();
-        const Tensor &x = saved[0], &stats = saved[1];
-        OptTensor w;
-        if (saved[2].defined()) w = saved[2];
-        const NormArguments a = {ctx->saved_data["eps"].toDouble(), ctx->saved_data["in"].toInt(),
-                                 ctx->saved_data["out"].toInt()};
-        // (an absent weight has no edge: the bias then comes second)
-        const bool need_dx = ctx->needs_input_grad(0), need_dw = w && ctx->needs_input_grad(1),
-                   need_db = ctx->saved_data["bias"].toBool() && ctx->needs_input_grad(w ? 2 : 1);
+        std::lock_guard<std::mutex> lock(mutex_);
+        TORCH_CHECK(!released, torch::autograd::ERR_BACKWARD_TWICE);
+        variable_list out(3);
         Tensor dy = grads[0];
+        if (!dy.defined()) return out;
+        const Tensor x = x_.unpack(), stats = stats_.unpack();
+        OptTensor w;
+        if (has_w) w = w_.unpack();
+        const bool need_dx = task_should_compute_output(0), need_dw = task_should_compute_output(1),
+                   need_db = task_should_compute_output(2);
         wtconv_norm_desc d;
-        bool ok = !twice(dy) && describe(x, a, d) && plain(stats, x.device()) && stats.is_contiguous() &&
-                  stats.scalar_type() == at::kFloat && stats.numel() == 2 * d.B * d.S &&
-                  vector_of(w, x.device(), d.C) && plain(dy, x.device()) && dy.scalar_type() == x.scalar_type() &&
-                  dy.sizes() == at::IntArrayRef(out_sizes(x, a));
-        const c10::OptionalDeviceGuard guard(x.device());
+        const bool ok = !twice(dy) && describe(x, args, d) && plain(stats, x.device()) && stats.is_contiguous() &&
+                        stats.scalar_type() == at::kFloat && stats.numel() == 2 * d.B * d.S &&
+                        vector_of(w, x.device(), d.C) && plain(dy, x.device()) &&
+                        dy.scalar_type() == x.scalar_type() && dy.sizes() == at::IntArrayRef(out_sizes(x, args));
         if (ok) {
-            if (a.out == 1) {
+            const c10::DeviceGuard guard(x.device());
+            if (args.out == 1) {
                 dy = dy.contiguous();
             } else if (!(d.dy_stride = row_stride(dy))) {
                 dy = dy.contiguous();
                 d.dy_stride = 0;
             }
-            variable_list out(6);
             if (need_dx) out[0] = at::empty(x.sizes(), x.options());
             if (need_dw) out[1] = floats({d.C}, x);
             if (need_db) out[2] = floats({d.C}, x);
             const size_t n = need_dw || need_db ? norm_bytes(&d) : 0;
             const Tensor ws = n ? bytes(n, x) : Tensor();
             const float* mean = stats.const_data_ptr<float>();
-            ok = norm_backward(&d, dy.const_data_ptr(), x.const_data_ptr(), mean, mean + d.B * d.S, ptr(w),
-                               need_dx ? out[0].mutable_data_ptr() : nullptr,
-                               need_dw ? out[1].mutable_data_ptr<float>() : nullptr,
-                               need_db ? out[2].mutable_data_ptr<float>() : nullptr,
-                               n ? ws.mutable_data_ptr() : nullptr, n, stream_of(x)) == WTCONV_OK;
-            if (ok) return out;
+            if (norm_backward(&d, dy.const_data_ptr(), x.const_data_ptr(), mean, mean + d.B * d.S, ptr(w),
+                              need_dx ? out[0].mutable_data_ptr() : nullptr,
+                              need_dw ? out[1].mutable_data_ptr<float>() : nullptr,
+                              need_db ? out[2].mutable_data_ptr<float>() : nullptr,
+                              n ? ws.mutable_data_ptr() : nullptr, n, stream_of(x)) == WTCONV_OK)
+                return out;
         }
         py::gil_scoped_acquire gil;
-        variable_list out = from_python(
-            python_norm, py::make_tuple(py::make_tuple(a.eps, a.in, a.out, need_dx, need_dw, need_db), grads[0], x,
-                                        stats.select(0, 0), stats.select(0, 1), w));
-        out.resize(6);
-        return out;
+        return from_python(python_norm,
+                           py::make_tuple(py::make_tuple(args.eps, args.in, args.out, need_dx, need_dw, need_db),
+                                          grads[0], x, stats.select(0, 0), stats.select(0, 1), w));
     }
 };
+
+Tensor norm_with_grad(const Tensor& x, const OptTensor& w, const OptTensor& b, const NormArguments& a)
+{
+    Tensor stats;
+    Tensor y = norm(x, w, b, a, &stats);
+    std::shared_ptr<NormNode> node(new NormNode(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(x, w ? *w : Tensor(), b ? *b : Tensor()));
+    node->x_ = SavedVariable(x, false);
+    node->stats_ = SavedVariable(stats, false);
+    if (w) node->w_ = SavedVariable(*w, false);
+    node->has_w = (bool)w;
+    node->args = a;
+    torch::autograd::set_history(y, node);
+    return y;
+}
 
 py::object layer_norm(py::handle x, py::handle weight, py::handle bias, py::handle eps, py::handle in, py::handle out)
 {
@@ -283,7 +302,7 @@ py::object layer_norm(py::handle x, py::handle weight, py::handle bias, py::hand
     Tensor y;
     try {
         py::gil_scoped_release no_gil;
-        y = grad ? NormFn::apply(xt, w, b, a.eps, a.in, a.out) : norm(xt, w, b, a, nullptr);
+        y = grad ? norm_with_grad(xt, w, b, a) : norm(xt, w, b, a, nullptr);
     } catch (const Refused&) {
         return py::none();  // the Python path raises the library's error
     }
@@ -332,52 +351,70 @@ Tensor residual(const Tensor& x, const Tensor& z, const OptTensor& gamma, const 
     return y;
 }
 
-struct ResidualFn : public torch::autograd::Function<ResidualFn> {
-    static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& z, const OptTensor& gamma,
-                          const OptTensor& keep, bool need_dgamma)
+struct ResidualNode : public Node {
+    SavedVariable z_, gamma_, keep_;
+    bool has_z = false, has_gamma = false, has_keep = false, released = false;
+
+    std::string name() const override { return "WTConvScaledResidual"; }
+    void release_variables() override
     {
-        Tensor y = residual(x, z, gamma, keep);
-        // z is needed for the gradient of gamma alone
-        ctx->save_for_backward({need_dgamma ? z : Tensor(), gamma ? *gamma : Tensor(), keep ? *keep : Tensor()});
-        return y;
+        std::lock_guard<std::mutex> lock(mutex_);
+        z_.reset_data();
+        gamma_.reset_data();
+        keep_.reset_data();
+        released = true;
     }
 
-    static variable_list backward(AutogradContext* ctx, variable_list grads)
+    variable_list apply(variable_list&& grads) override
     {
-        const variable_list saved = ctx->get_saved_variables();
-        const Tensor& z = saved[0];
-        OptTensor gamma, keep;
-        if (saved[1].defined()) gamma = saved[1];
-        if (saved[2].defined()) keep = saved[2];
-        const bool need_dx = ctx->needs_input_grad(0), need_dz = ctx->needs_input_grad(1),
-                   need_dg = gamma && z.defined() && ctx->needs_input_grad(2);
+        std::lock_guard<std::mutex> lock(mutex_);
+        TORCH_CHECK(!released, torch::autograd::ERR_BACKWARD_TWICE);
+        variable_list out(3);
+        if (!grads[0].defined()) return out;
+        OptTensor z, gamma, keep;
+        if (has_z) z = z_.unpack();
+        if (has_gamma) gamma = gamma_.unpack();
+        if (has_keep) keep = keep_.unpack();
+        const bool need_dx = task_should_compute_output(0), need_dz = task_should_compute_output(1),
+                   need_dg = z && task_should_compute_output(2);
         const bool second = twice(grads[0]);
         const Tensor dy = second ? grads[0] : grads[0].contiguous();
-        const c10::OptionalDeviceGuard guard(dy.device());
         wtconv_residual_desc d;
         if (!second && describe(dy, d) && vector_of(gamma, dy.device(), d.C) && vector_of(keep, dy.device(), d.B) &&
-            (!need_dg || rows_of(z, dy))) {
-            variable_list out(5);
+            (!need_dg || rows_of(*z, dy))) {
+            const c10::DeviceGuard guard(dy.device());
             if (need_dx) out[0] = dy;
             if (need_dz) out[1] = at::empty(rows_sizes(dy), dy.options());
             if (need_dg) out[2] = floats({d.C}, dy);
             const size_t n = need_dg ? residual_bytes(&d) : 0;
             const Tensor ws = n ? bytes(n, dy) : Tensor();
-            if (residual_backward(&d, dy.const_data_ptr(), need_dg ? z.const_data_ptr() : nullptr, ptr(gamma),
+            if (residual_backward(&d, dy.const_data_ptr(), need_dg ? z->const_data_ptr() : nullptr, ptr(gamma),
                                   ptr(keep), need_dz ? out[1].mutable_data_ptr() : nullptr,
                                   need_dg ? out[2].mutable_data_ptr<float>() : nullptr,
                                   n ? ws.mutable_data_ptr() : nullptr, n, stream_of(dy)) == WTCONV_OK)
                 return out;
         }
         py::gil_scoped_acquire gil;
-        OptTensor zo;
-        if (z.defined()) zo = z;
-        variable_list out = from_python(
-            python_residual, py::make_tuple(py::make_tuple(need_dx, need_dz, need_dg), grads[0], zo, gamma, keep));
-        out.resize(5);
-        return out;
+        return from_python(python_residual,
+                           py::make_tuple(py::make_tuple(need_dx, need_dz, need_dg), grads[0], z, gamma, keep));
     }
 };
+
+Tensor residual_with_grad(const Tensor& x, const Tensor& z, const OptTensor& gamma, const OptTensor& keep)
+{
+    Tensor y = residual(x, z, gamma, keep);
+    std::shared_ptr<ResidualNode> node(new ResidualNode(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(x, z, gamma ? *gamma : Tensor()));
+    // z is needed for the gradient of gamma alone
+    node->has_z = gamma && gamma->requires_grad();
+    if (node->has_z) node->z_ = SavedVariable(z, false);
+    node->has_gamma = (bool)gamma;
+    if (gamma) node->gamma_ = SavedVariable(*gamma, false);
+    node->has_keep = (bool)keep;
+    if (keep) node->keep_ = SavedVariable(*keep, false);
+    torch::autograd::set_history(y, node);
+    return y;
+}
 
 py::object scaled_residual(py::handle x, py::handle z, py::handle gamma, py::handle keep)
 {
@@ -389,12 +426,12 @@ py::object scaled_residual(py::handle x, py::handle z, py::handle gamma, py::han
     if (!describe(xt, d) || !rows_of(zt, xt) || !vector_of(g, xt.device(), d.C) || !vector_of(k, xt.device(), d.B) ||
         (k && k->requires_grad()))
         return py::none();
-    const bool dg = g && g->requires_grad();
-    const bool grad = at::GradMode::is_enabled() && (xt.requires_grad() || zt.requires_grad() || dg);
+    const bool grad = at::GradMode::is_enabled() &&
+                      (xt.requires_grad() || zt.requires_grad() || (g && g->requires_grad()));
     Tensor y;
     try {
         py::gil_scoped_release no_gil;
-        y = grad ? ResidualFn::apply(xt, zt, g, k, dg) : residual(xt, zt, g, k);
+        y = grad ? residual_with_grad(xt, zt, g, k) : residual(xt, zt, g, k);
     } catch (const Refused&) {
         return py::none();
     }
@@ -460,7 +497,7 @@ bool adamw_step(const std::vector<Group*>& plans, py::sequence params, const std
             const Tensor& g = p.grad();
             if (!g.defined()) continue;
             wtconv_dtype type;
-            if (!plain(p, q.m.device()) || !plain(g, q.m.device()) || !type_of(p, type) ||
+            if (!plain(p, q.m.device(), false) || !plain(g, q.m.device(), false) || !type_of(p, type) ||
                 g.scalar_type() != p.scalar_type() || p.numel() != q.numel[i] || g.sizes() != p.sizes() ||
                 g.strides() != p.strides() || !p.is_non_overlapping_and_dense() || p.is_inference())
                 return false;
@@ -512,9 +549,25 @@ bool adamw_step(const std::vector<Group*>& plans, py::sequence params, const std
     return true;
 }
 
+// The values of a group's 8-bit moments, or None.
+py::object adamw_moments(const Group& q, at::ScalarType type)
+{
+    wtconv_dtype d;
+    if (!moments_fn || !q.ms || !q.vs || modes_active()) return py::none();
+    const c10::DeviceGuard guard(q.m.device());
+    const auto options = q.m.options().dtype(type);
+    Tensor m = at::empty(q.m.sizes(), options), v = at::empty(q.m.sizes(), options);
+    if (!type_of(m, d) ||
+        moments_fn(q.m.numel(), q.m.const_data_ptr<uint8_t>(), q.ms->const_data_ptr<uint8_t>(),
+                   q.v.const_data_ptr<uint8_t>(), q.vs->const_data_ptr<uint8_t>(), m.mutable_data_ptr(),
+                   v.mutable_data_ptr(), d, stream_of(m)) != WTCONV_OK)
+        return py::none();
+    return py::make_tuple(m, v);
+}
+
 void init(const std::vector<uintptr_t>& fns, py::object norm_py, py::object residual_py)
 {
-    TORCH_CHECK(fns.size() == 7, "init takes the addresses of seven entry points");
+    TORCH_CHECK(fns.size() == 8, "init takes the addresses of eight entry points");
     norm_forward = reinterpret_cast<decltype(norm_forward)>(fns[0]);
     norm_bytes = reinterpret_cast<decltype(norm_bytes)>(fns[1]);
     norm_backward = reinterpret_cast<decltype(norm_backward)>(fns[2]);
@@ -522,6 +575,7 @@ void init(const std::vector<uintptr_t>& fns, py::object norm_py, py::object resi
     residual_bytes = reinterpret_cast<decltype(residual_bytes)>(fns[4]);
     residual_backward = reinterpret_cast<decltype(residual_backward)>(fns[5]);
     adamw_fn = reinterpret_cast<decltype(adamw_fn)>(fns[6]);
+    moments_fn = reinterpret_cast<decltype(moments_fn)>(fns[7]);
     py::object parameter = py::module_::import("torch.nn").attr("Parameter");
     parameter_type = reinterpret_cast<PyTypeObject*>(parameter.release().ptr());
     Py_XDECREF(python_norm);
@@ -540,4 +594,5 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
     m.def("layer_norm", &layer_norm);
     m.def("scaled_residual", &scaled_residual);
     m.def("adamw_step", &adamw_step);
+    m.def("adamw_moments", &adamw_moments);
 }

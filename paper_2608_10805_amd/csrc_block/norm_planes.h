@@ -67,12 +67,18 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     const uint32_t tile = kShared ? follow(blockIdx.x, gridDim.x) : blockIdx.x;
     if (tile >= ps.tiles) return;
     const Place<Ti> at(ps, tile, px, slot);
-    float v[K][V][G], s[V] = {}, mean[V], rstd[V];
+    float v[K][V][G], w[K][G], b[K][G], s[V] = {}, mean[V], rstd[V];
     int left[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         left[k] = at.left(a.C, slot, k);
         load_pixels<Ti>((const T*)a.x, at, a.S, left[k], k, v[k]);
+    }
+    // on their way behind x, and here before the sums need them
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        load_channels<G>(a.w, (k * NS + slot) * G, a.C, 1.0f, w[k]);
+        load_channels<G>(a.b, (k * NS + slot) * G, a.C, 0.0f, b[k]);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
@@ -107,13 +113,10 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         if (left[k] <= 0) continue;
-        float w[G], b[G];
-        load_channels<G>(a.w, (k * NS + slot) * G, a.C, 1.0f, w);
-        load_channels<G>(a.b, (k * NS + slot) * G, a.C, 0.0f, b);
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll
-            for (int g = 0; g < G; ++g) v[k][i][g] = v[k][i][g] * rstd[i] * w[g] + b[g];
+            for (int g = 0; g < G; ++g) v[k][i][g] = v[k][i][g] * rstd[i] * w[k][g] + b[k][g];
         if (OUT_PLANES) store_pixels<Ti>((T*)a.out, at, a.S, left[k], k, v[k]);
     }
     if constexpr (!OUT_PLANES) {

@@ -172,8 +172,12 @@ class AdamW(torch.optim.Optimizer):
         tensors of `dtype` (bfloat16 holds each exactly down to 2^-126)."""
         if self.state_bits == 32:
             return [(b["exp_avg"], b["exp_avg_sq"]) for b in self._buffers]
-        return [binding.adamw_moments(b["exp_avg"], b["exp_avg_scale"], b["exp_avg_sq"], b["exp_avg_sq_scale"], dtype)
-                for b in self._buffers]
+        if dtype not in _DTYPES:
+            raise ValueError(f"the moments' values are float32, bfloat16 or float16, not {dtype}")
+        ext = autograd._block
+        return [ext and native and ext.adamw_moments(native, dtype) or
+                binding.adamw_moments(b["exp_avg"], b["exp_avg_scale"], b["exp_avg_sq"], b["exp_avg_sq_scale"], dtype)
+                for b, native in zip(self._buffers, self._native)]
 
     def load_state_dict(self, state_dict):
         """Copy the hyperparameters and the moments of a state_dict() of an optimizer with the same groups, shapes and

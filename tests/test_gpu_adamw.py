@@ -230,6 +230,9 @@ def test_the_native_host_path_is_the_python_one(bits, monkeypatch):
             monkeypatch.setattr(opt, "_step", lambda scale: pytest.fail("left to Python"))
         else:
             opt._native = [None] * 2
+            if bits == 8:
+                with pytest.raises(ValueError, match="float32, bfloat16"):
+                    opt.moments(torch.float64)
         for _ in range(2):
             opt.step(grad_scale=torch.tensor(0.5, device=DEV))
         runs.append([p.detach().clone() for p in ps] + [t for pair in opt.moments() for t in pair] +
