@@ -82,10 +82,12 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        over_channels<Ti>(left[k], [&](int g) ALWAYS {
+        if (left[k] > 0) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[i] += v[k][i][g];
-        });
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int g = 0; g < G; ++g) s[i] += v[k][i][g];
+        }
     slot_sum<Ti>(s, red[0]);
     const float per = 1.0f / a.C;
 #pragma unroll
@@ -96,13 +98,15 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     // the variance from the centred values, which are at hand: no cancellation
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        over_channels<Ti>(left[k], [&](int g) ALWAYS {
+        if (left[k] > 0) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                v[k][i][g] -= mean[i];
-                s[i] += v[k][i][g] * v[k][i][g];
-            }
-        });
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    v[k][i][g] = Ti::kRegular || g < left[k] ? v[k][i][g] - mean[i] : 0.f;
+                    s[i] += v[k][i][g] * v[k][i][g];
+                }
+        }
     slot_sum<Ti>(s, red[1]);
 #pragma unroll
     for (int i = 0; i < V; ++i) rstd[i] = 1.0f / sqrtf(s[i] * per + a.eps);
@@ -181,9 +185,12 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
         }
 #pragma unroll
         for (int k = 0; k < K; ++k) {
+            // (a channel that is not there has dy = 0: it adds nothing to any sum)
+            if (left[k] <= 0) continue;
             float w[G];
-            if (left[k] > 0) load_channels<G>(a.w, (k * NS + slot) * G, a.C, 1.0f, w);
-            over_channels<Ti>(left[k], [&](int j) ALWAYS {
+            load_channels<G>(a.w, (k * NS + slot) * G, a.C, 1.0f, w);
+#pragma unroll
+            for (int j = 0; j < G; ++j)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     xhat[k][i][j] = (xhat[k][i][j] - mean[i]) * rstd[i];
@@ -193,7 +200,6 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
                     s1[i] += g[k][i][j];
                     s2[i] += g[k][i][j] * xhat[k][i][j];
                 }
-            });
         }
         if (!a.out) continue;
         __syncthreads();  // the last tile's sums have been read
@@ -206,10 +212,13 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
         }
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            over_channels<Ti>(left[k], [&](int j) ALWAYS {
+            if (left[k] > 0) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) g[k][i][j] = rstd[i] * g[k][i][j] - s1[i] - xhat[k][i][j] * s2[i];
-            });
+                for (int i = 0; i < V; ++i)
+#pragma unroll
+                    for (int j = 0; j < G; ++j)
+                        g[k][i][j] = rstd[i] * g[k][i][j] - s1[i] - xhat[k][i][j] * s2[i];
+            }
             store_pixels<Ti>((T*)a.out, at, a.S, left[k], k, g[k]);
         }
     }
@@ -249,6 +258,7 @@ bool planes_tile(int index, F&& f)
             WTC_TILE(6, 192, 4, 2);
             WTC_TILE(7, 256, 4, 3);
             WTC_TILE(8, 512, 4, 3);
+            WTC_TILE(9, 512, 2, 2);
         }
     } else if constexpr (V == 4) {
         switch (index) {
@@ -260,7 +270,7 @@ bool planes_tile(int index, F&& f)
             WTC_TILE(5, 256, 4, 1);
             WTC_TILE(6, 384, 4, 1);
             WTC_TILE(7, 512, 4, 1);
-            WTC_TILE(8, 768, 4, 1);
+            WTC_TILE(8, 512, 2, 1);
         }
     } else {
         constexpr int E = 4 / sizeof(T);  // twice the channels a unit, half the steps
@@ -269,7 +279,7 @@ bool planes_tile(int index, F&& f)
             WTC_TILE(1, 256, 32, E == 1 ? 6 : 3);
             WTC_TILE(2, 256, 16, E == 1 ? 6 : 3);
             WTC_TILE(3, 512, 16, E == 1 ? 6 : 3);
-            WTC_TILE(4, 1024, 16, E == 1 ? 6 : 3);
+            WTC_TILE(4, 512, 8, E == 1 ? 8 : 4);
         }
     }
 #undef WTC_TILE
@@ -308,11 +318,36 @@ int pick_tile(int64_t B, int64_t S, int C, double& best_score)
     return best;
 }
 
-template <typename T, int V, bool REGULAR>
-bool planes_launch(int index, bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
+// Calls f with the tile for these planes, false where there is none: vectors of
+// four pixels, but for images so small that most of them would be incomplete
+// (single pixels then run over all images).
+template <typename T, typename F>
+bool with_tile(int64_t B, int64_t S, int C, F&& f)
+{
+    double fours = 0, ones = 0;
+    if (S % 4 == 0 && C % (16 / (int)sizeof(T)) == 0) return planes_tile<T, 4, true>(pick_tile<T, 4, true>(B, S, C, fours), f);
+    const int i = pick_tile<T, 4, false>(B, S, C, fours), j = pick_tile<T, 1, false>(B, S, C, ones);
+    return fours >= 0.5 * ones ? planes_tile<T, 4, false>(i, f) : planes_tile<T, 1, false>(j, f);
+}
+
+// Workgroups of the backward pass: no more than tiles.
+template <typename T>
+int64_t planes_tiles(int64_t B, int64_t S, int C)
+{
+    int64_t n = 0;
+    with_tile<T>(B, S, C, [&](auto t) {
+        Pixels ps;
+        if (pixels_of<decltype(t)>(B, S, C, ps)) n = ps.tiles;
+    });
+    return n;
+}
+
+// x and dx are planes, and y or dy if `out_planes`.
+template <typename T>
+bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
 {
     bool done = false;
-    planes_tile<T, V, REGULAR>(index, [&](auto t) {
+    with_tile<T>(a.B, a.S, a.C, [&](auto t) {
         using Ti = decltype(t);
         Pixels ps;
         if (!pixels_of<Ti>(a.B, a.S, a.C, ps)) return;
@@ -328,22 +363,6 @@ bool planes_launch(int index, bool forward, bool out_planes, const NormArgs& a, 
             hipLaunchKernelGGL((planes_backward<Ti, false>), grid, block, 0, s, a, ps);
     });
     return done;
-}
-
-// x and dx are planes, and y or dy if `out_planes`. Vectors of four pixels, but
-// for images so small that most of them would be incomplete: single pixels then
-// run over all images.
-template <typename T>
-bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t s)
-{
-    double fours = 0, ones = 0;
-    if (a.S % 4 == 0 && a.C % (16 / (int)sizeof(T)) == 0) {
-        const int i = pick_tile<T, 4, true>(a.B, a.S, a.C, fours);
-        return planes_launch<T, 4, true>(i, forward, out_planes, a, s);
-    }
-    const int i = pick_tile<T, 4, false>(a.B, a.S, a.C, fours), j = pick_tile<T, 1, false>(a.B, a.S, a.C, ones);
-    if (fours >= 0.5 * ones && planes_launch<T, 4, false>(i, forward, out_planes, a, s)) return true;
-    return planes_launch<T, 1, false>(j, forward, out_planes, a, s);
 }
 
 }  // namespace wtc

@@ -176,13 +176,13 @@ __global__ void __launch_bounds__(Ti::TH) residual_backward(const ResidualArgs a
             float z[V][G], scale[G];
             if (a.part) Tu::get(turn, px, k * NS + slot, z);
             channel_factors<G>(a.gamma, c0 + (k * NS + slot) * G, left[k], scale);
-            over_channels<Ti>(left[k], [&](int g) ALWAYS {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    if (a.part) sum[k][g] += d[k][i][g] * z[i][g] * keep;
+                    if (a.part) sum[k][g] += d[k][i][g] * z[i][g] * keep;  // (both zero past the end)
                     d[k][i][g] *= scale[g] * keep;
                 }
-            });
             if (a.out) Tu::put(turn, px, k * NS + slot, d[k]);
         }
         __syncthreads();

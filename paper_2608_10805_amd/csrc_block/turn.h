@@ -206,43 +206,70 @@ struct Place {
     }
 };
 
-// Calls f(g) for each channel of a thread's unit that there is.
-template <typename Ti, typename F>
-DEV void over_channels(int left, F&& f)
-{
-    if constexpr (Ti::kRegular) {
-        if (left > 0) {
-#pragma unroll
-            for (int g = 0; g < Ti::G; ++g) f(g);
-        }
-    } else {
-#pragma unroll
-        for (int g = 0; g < Ti::G; ++g)
-            if (g < left) f(g);
-    }
-}
+// Keeps the compiler from joining the common end of two branches into one that
+// goes over arrays by an index (which puts them into memory).
+#define APART asm volatile("")
 
-// The thread's pixels of its unit of step k; zeros for pixels that are not
-// there, nothing for channels.
+// Whether a wavefront's units are all whole, or not there: one test for all of
+// their channels then.
+template <typename Ti>
+DEV bool all_whole(int left) { return Ti::kRegular || !__any(left > 0 && left < Ti::G); }
+
+// The thread's pixels of its unit of step k, if there is one; zeros for pixels
+// and for channels that are not there.
 template <typename Ti, typename T = typename Ti::Type>
 DEV void load_pixels(const T* p, const Place<Ti>& at, int64_t S, int left, int k, float (&f)[Ti::V][Ti::G])
 {
-    over_channels<Ti>(left, [&](int g) ALWAYS {
-        const auto q = load_upto<Ti::V>(at.at(p, S, k, g), Ti::kFlat ? Ti::V : at.count);
+    const auto load = [&](int g, bool there) ALWAYS {
+        Pack<T, Ti::V> q;
+        if (Ti::kFlat || at.rows == Ti::P) {
+#pragma unroll
+            for (int i = 0; i < Ti::V; ++i) q.v[i] = T(0);
+            if (there) q = load_pack<Ti::V>(at.at(p, S, k, g));
+        } else {
+            q = load_upto<Ti::V>(at.at(p, S, k, g), there ? at.count : 0);
+            APART;
+        }
 #pragma unroll
         for (int i = 0; i < Ti::V; ++i) f[i][g] = to_f32(q.v[i]);
-    });
+    };
+    if (all_whole<Ti>(left)) {
+        if (left > 0) {
+#pragma unroll
+            for (int g = 0; g < Ti::G; ++g) load(g, true);
+        }
+    } else {
+#pragma unroll
+        for (int g = 0; g < Ti::G; ++g) load(g, g < left);
+        APART;
+    }
 }
 
 template <typename Ti, typename T = typename Ti::Type>
 DEV void store_pixels(T* p, const Place<Ti>& at, int64_t S, int left, int k, const float (&f)[Ti::V][Ti::G])
 {
-    over_channels<Ti>(left, [&](int g) ALWAYS {
+    const auto store = [&](int g) ALWAYS {
         Pack<T, Ti::V> q;
 #pragma unroll
         for (int i = 0; i < Ti::V; ++i) q.v[i] = from_f32<T>(f[i][g]);
-        store_upto<Ti::V>(at.at(p, S, k, g), Ti::kFlat ? Ti::V : at.count, q);
-    });
+        if (Ti::kFlat || at.rows == Ti::P) {
+            store_pack<Ti::V>(at.at(p, S, k, g), q);
+        } else {
+            store_upto<Ti::V>(at.at(p, S, k, g), at.count, q);
+            APART;
+        }
+    };
+    if (all_whole<Ti>(left)) {
+        if (left > 0) {
+#pragma unroll
+            for (int g = 0; g < Ti::G; ++g) store(g);
+        }
+    } else {
+#pragma unroll
+        for (int g = 0; g < Ti::G; ++g)
+            if (g < left) store(g);
+        APART;
+    }
 }
 
 }  // namespace wtc
