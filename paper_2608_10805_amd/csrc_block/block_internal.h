@@ -74,8 +74,8 @@ bool launch_rows_backward(wtconv_dtype dt, const NormArgs& a, hipStream_t s);
 bool launch_planes_f32(bool forward, bool out_planes, const NormArgs& a, hipStream_t s);
 bool launch_planes_bf16(bool forward, bool out_planes, const NormArgs& a, hipStream_t s);
 bool launch_planes_f16(bool forward, bool out_planes, const NormArgs& a, hipStream_t s);
-int64_t tiles_planes_f32(int64_t B, int64_t S, int C);  // 0 where there are none
-int64_t tiles_planes_16(int64_t B, int64_t S, int C);
+int64_t parts_planes_f32(int64_t B, int64_t S, int C);  // workgroups of the backward pass, 0 where it is not theirs
+int64_t parts_planes_16(int64_t B, int64_t S, int C);
 hipError_t launch_norm_forward(const wtconv_norm_desc& d, const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_backward(const wtconv_norm_desc& d, NormArgs a, float* dw, float* db, hipStream_t s);
 hipError_t launch_residual_forward(wtconv_dtype dt, const ResidualArgs& a, hipStream_t s);

@@ -320,16 +320,15 @@ bool launch_planes(bool forward, const wtconv_norm_desc& d, const NormArgs& a, h
 
 }  // namespace
 
-// Four workgroups a CU, half of that where their sums are long (2047 bfloat16
-// channels, 4096 rows: 61.0 us with 1024, 42.8 with 512), and no more than there
-// are tiles of planes or 16 rows.
+// Of rows, and of planes that the kernels here take: four workgroups a CU, half
+// of that where their sums are long (2047 bfloat16 channels, 4096 rows: 61.0 us
+// with 1024, 42.8 with 512), and no more than there are 16 rows.
 int64_t norm_parts(const wtconv_norm_desc& d)
 {
-    int64_t tiles = 0;
+    int64_t parts = 0;
     if (d.in == WTCONV_PLANES && d.B && d.S)
-        tiles = (d.dtype == WTCONV_F32 ? tiles_planes_f32 : tiles_planes_16)(d.B, d.S, d.C);
-    if (!tiles) tiles = (d.B * d.S + 15) / 16;
-    return at_most(tiles, d.C > 1024 ? 512 : 1024);
+        parts = (d.dtype == WTCONV_F32 ? parts_planes_f32 : parts_planes_16)(d.B, d.S, d.C);
+    return parts ? parts : at_most((d.B * d.S + 15) / 16, d.C > 1024 ? 512 : 1024);
 }
 
 hipError_t launch_sum_parts(const float* part, int64_t rows, int width, int half, float* out, float* out2,

@@ -104,6 +104,22 @@ DEV float sum_within(float v, int n)
 // other, and tiles that share lines of memory share an L2.
 DEV uint32_t follow(uint32_t block, uint32_t n) { return (block & 7) * (n >> 3) + (block >> 3); }
 
+// s / n for a whole n with 1 / n at hand: correctly rounded but for rare cases of
+// half a unit (a constant row's mean is its value).
+DEV float divided(float s, float n, float per)
+{
+    const float q = s * per;
+    return __builtin_fmaf(__builtin_fmaf(-q, n, s), per, q);
+}
+
+// 1 / sqrt(v), the hardware's approximation and one Newton step. Every lane of a
+// pixel computes it, so the library's exact steps would cost more than the sums.
+DEV float inverse_root(float v)
+{
+    const float r = __builtin_amdgcn_rsqf(v);
+    return __builtin_fmaf(0.5f * __builtin_fmaf(-v * r, r, 1.0f), r, r);
+}
+
 inline int at_most(int64_t items, int64_t most) { return (int)(items < most ? (items > 1 ? items : 1) : most); }
 
 }  // namespace wtc

@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     const float per = 1.0f / a.C;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        mean[i] = s[i] / a.C;  // (exact for a constant pixel)
+        mean[i] = divided(s[i], (float)a.C, per);
         s[i] = 0.f;
     }
     // the variance from the centred values, which are at hand: no cancellation
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
         }
     slot_sum<Ti>(s, red[1]);
 #pragma unroll
-    for (int i = 0; i < V; ++i) rstd[i] = 1.0f / sqrtf(s[i] * per + a.eps);
+    for (int i = 0; i < V; ++i) rstd[i] = inverse_root(s[i] * per + a.eps);
     if (a.mean && slot == 0) {
         store_upto<V>(a.mean + at.q, at.count, __builtin_bit_cast(Pack<float, V>, mean));
         store_upto<V>(a.rstd + at.q, at.count, __builtin_bit_cast(Pack<float, V>, rstd));
@@ -259,6 +259,8 @@ bool planes_tile(int index, F&& f)
             WTC_TILE(7, 256, 4, 3);
             WTC_TILE(8, 512, 4, 3);
             WTC_TILE(9, 512, 2, 2);
+            WTC_TILE(10, 64, 16, 2);
+            WTC_TILE(11, 128, 16, 2);
         }
     } else if constexpr (V == 4) {
         switch (index) {
@@ -271,6 +273,9 @@ bool planes_tile(int index, F&& f)
             WTC_TILE(6, 384, 4, 1);
             WTC_TILE(7, 512, 4, 1);
             WTC_TILE(8, 512, 2, 1);
+            WTC_TILE(9, 64, 16, 1);
+            WTC_TILE(10, 128, 16, 1);
+            WTC_TILE(11, 512, 8, 2);
         }
     } else {
         constexpr int E = 4 / sizeof(T);  // twice the channels a unit, half the steps
@@ -330,14 +335,22 @@ bool with_tile(int64_t B, int64_t S, int C, F&& f)
     return fours >= 0.5 * ones ? planes_tile<T, 4, false>(i, f) : planes_tile<T, 1, false>(j, f);
 }
 
-// Workgroups of the backward pass: no more than tiles.
+// Workgroups of the backward pass: as many as are resident by the registers that
+// their threads' values take, no more than there are tiles. What each adds is 2 C
+// sums to write and to read again, so that many channels get four a CU at most.
+// Measured on 384 bfloat16 channels, 14 x 14, B128: tiles of 192 threads 48.2,
+// 35.6, 34.8 us with 256, 512, 1024 workgroups, tiles of 512 threads 44.0, 46.5,
+// 55.6 us.
 template <typename T>
-int64_t planes_tiles(int64_t B, int64_t S, int C)
+int64_t planes_parts(int64_t B, int64_t S, int C)
 {
     int64_t n = 0;
     with_tile<T>(B, S, C, [&](auto t) {
+        using Ti = decltype(t);
         Pixels ps;
-        if (pixels_of<decltype(t)>(B, S, C, ps)) n = ps.tiles;
+        if (!pixels_of<Ti>(B, S, C, ps)) return;
+        const int resident = 24576 / (Ti::TH * Ti::K * Ti::V * Ti::G), few = C <= 32 ? 12 : C <= 64 ? 6 : 4;
+        n = at_most(ps.tiles, 256 * (resident < 1 ? 1 : resident < few ? resident : few));
     });
     return n;
 }

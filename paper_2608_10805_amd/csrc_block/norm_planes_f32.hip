@@ -8,6 +8,6 @@ bool launch_planes_f32(bool forward, bool out_planes, const NormArgs& a, hipStre
     return planes_launch<float>(forward, out_planes, a, s);
 }
 
-int64_t tiles_planes_f32(int64_t B, int64_t S, int C) { return planes_tiles<float>(B, S, C); }
+int64_t parts_planes_f32(int64_t B, int64_t S, int C) { return planes_parts<float>(B, S, C); }
 
 }  // namespace wtc

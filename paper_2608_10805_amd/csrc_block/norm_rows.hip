@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kThreads) rows_forward(const NormArgs a, int g
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int i = 0; i < V; ++i) s += v[r][i];
-    const float per = 1.0f / a.C, mean = sum_within(s, gl) / a.C;  // (exact for a constant pixel)
+    const float per = 1.0f / a.C, mean = divided(sum_within(s, gl), (float)a.C, per);
     s = 0.f;
     // the variance from the centred values, which are at hand: no cancellation
 #pragma unroll
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(kThreads) rows_forward(const NormArgs a, int g
             s += v[r][i] * v[r][i];
         }
     }
-    const float rstd = 1.0f / sqrtf(sum_within(s, gl) * per + a.eps);
+    const float rstd = inverse_root(sum_within(s, gl) * per + a.eps);
     if (a.mean && lane == 0) {
         a.mean[q] = mean;
         a.rstd[q] = rstd;

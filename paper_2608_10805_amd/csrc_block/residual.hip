@@ -203,9 +203,14 @@ __global__ void __launch_bounds__(Ti::TH) residual_backward(const ResidualArgs a
         }
 }
 
-// Channels of a block: 96 or 128, whichever leaves fewer lanes idle in the last
-// one (96 and its multiples are this kind of network's widths).
-int block_channels(int C) { return (C + 95) / 96 * 96 < (C + 127) / 128 * 128 ? 96 : 128; }
+// Channels of a block: the widest of those that leave the fewest lanes idle in
+// the last one (32 and 64 where there are no more).
+int block_channels(int C)
+{
+    if (C <= 32) return 32;
+    if (C <= 64) return 64;
+    return (C + 95) / 96 * 96 < (C + 127) / 128 * 128 ? 96 : 128;
+}
 
 template <typename Ti>
 bool launch(bool forward, const ResidualArgs& a, hipStream_t s)
@@ -224,12 +229,12 @@ template <typename T, int V, bool REGULAR>
 bool launch_tile(bool forward, const ResidualArgs& a, hipStream_t s)
 {
     constexpr int E = sizeof(T) / 2;  // 16-byte units of float32 hold half the channels: twice the steps
-    if constexpr (V == 4) {
-        if (block_channels(a.C) == 96) return launch<Tile<T, 192, 4, 16, E, REGULAR>>(forward, a, s);
-        return launch<Tile<T, 256, 4, 16, E, REGULAR>>(forward, a, s);
-    } else {
-        if (block_channels(a.C) == 96) return launch<Tile<T, 192, 1, 64, 4 * E, false>>(forward, a, s);
-        return launch<Tile<T, 256, 1, 64, 4 * E, false>>(forward, a, s);
+    constexpr int LP = V == 4 ? 16 : 64, K = V == 4 ? E : 4 * E;
+    switch (block_channels(a.C)) {
+        case 32: return launch<Tile<T, 64, V, LP, K, REGULAR>>(forward, a, s);
+        case 64: return launch<Tile<T, 128, V, LP, K, REGULAR>>(forward, a, s);
+        case 96: return launch<Tile<T, 192, V, LP, K, REGULAR>>(forward, a, s);
+        default: return launch<Tile<T, 256, V, LP, K, REGULAR>>(forward, a, s);
     }
 }
 
@@ -268,11 +273,11 @@ hipError_t launch_type(wtconv_dtype dt, bool forward, const ResidualArgs& a, hip
 
 }  // namespace
 
-// Four workgroups a CU over all blocks of channels.
+// 16 wavefronts a CU over all blocks of channels.
 int64_t residual_parts(const wtconv_residual_desc& d)
 {
-    const int64_t blocks = (d.C + block_channels(d.C) - 1) / block_channels(d.C);
-    return at_most((d.B * d.S + kTile - 1) / kTile, blocks < 16 ? 1024 / blocks : 64);
+    const int64_t width = block_channels(d.C), blocks = (d.C + width - 1) / width, parts = 4096 / (width / 32) / blocks;
+    return at_most((d.B * d.S + kTile - 1) / kTile, parts < 64 ? 64 : parts);
 }
 
 hipError_t launch_residual_forward(wtconv_dtype dt, const ResidualArgs& a, hipStream_t s)
