@@ -60,11 +60,10 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     using T = typename Ti::Type;
     using Tu = Turn<Ti>;
     constexpr int V = Ti::V, NS = Ti::NS, K = Ti::K, G = Ti::G;
-    constexpr bool kShared = Ti::P * sizeof(T) < 128;  // tiles side by side share lines of memory
     __shared__ float red[2][Ti::NW][Ti::P];
     __shared__ uint4 turn[OUT_PLANES ? 1 : Tu::kSize];
     const int px = threadIdx.x % Ti::LP, slot = threadIdx.x / Ti::LP;
-    const uint32_t tile = kShared ? follow(blockIdx.x, gridDim.x) : blockIdx.x;
+    const uint32_t tile = Ti::kShared ? follow(blockIdx.x, gridDim.x) : blockIdx.x;
     if (tile >= ps.tiles) return;
     const Place<Ti> at(ps, tile, px, slot);
     float v[K][V][G], w[K][G], b[K][G], s[V] = {}, mean[V], rstd[V];
@@ -145,13 +144,12 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
     using T = typename Ti::Type;
     using Tu = Turn<Ti>;
     constexpr int V = Ti::V, NS = Ti::NS, K = Ti::K, G = Ti::G;
-    constexpr bool kShared = Ti::P * sizeof(T) < 128;  // tiles side by side share lines of memory
     __shared__ float red[2][Ti::NW][Ti::P];
     __shared__ uint4 turn[OUT_PLANES ? 1 : Tu::kSize];
     const int px = threadIdx.x % Ti::LP, slot = threadIdx.x / Ti::LP;
     const float per = 1.0f / a.C;
     float sw[K][G] = {}, sb[K][G] = {};
-    const uint32_t first = !kShared || gridDim.x % 8 ? blockIdx.x : follow(blockIdx.x, gridDim.x);
+    const uint32_t first = !Ti::kShared || gridDim.x % 8 ? blockIdx.x : follow(blockIdx.x, gridDim.x);
     for (uint32_t tile = first; tile < ps.tiles; tile += gridDim.x) {
         const Place<Ti> at(ps, tile, px, slot);
         float xhat[K][V][G], g[K][V][G], s1[V] = {}, s2[V] = {}, mean[V], rstd[V];
@@ -276,6 +274,7 @@ bool planes_tile(int index, F&& f)
             WTC_TILE(9, 64, 16, 1);
             WTC_TILE(10, 128, 16, 1);
             WTC_TILE(11, 512, 8, 2);
+            WTC_TILE(12, 384, 8, 1);
         }
     } else {
         constexpr int E = 4 / sizeof(T);  // twice the channels a unit, half the steps

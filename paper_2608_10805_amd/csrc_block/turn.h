@@ -25,6 +25,8 @@ struct Tile {
     // the next, else over each image's by itself.
     static constexpr bool kFlat = REGULAR || V == 1;
     static constexpr int P = LP * V, NS = TH / LP, NW = TH / 64;
+    // Tiles side by side share lines of 128 bytes.
+    static constexpr bool kShared = !REGULAR || P * sizeof(T) < 128;
     static constexpr int kChannels = NS * G;       // channels of one step k
     static constexpr int kMaxC = kChannels * K;
     static_assert(NW * 64 == TH && NS * LP == TH && (LP & (LP - 1)) == 0 && (V & (V - 1)) == 0, "whole wavefronts");
