@@ -269,12 +269,12 @@ bool planes_tile(int index, F&& f)
             WTC_TILE(4, 192, 4, 1);
             WTC_TILE(5, 256, 4, 1);
             WTC_TILE(6, 384, 4, 1);
-            WTC_TILE(7, 512, 4, 1);
-            WTC_TILE(8, 512, 2, 1);
-            WTC_TILE(9, 64, 16, 1);
-            WTC_TILE(10, 128, 16, 1);
-            WTC_TILE(11, 512, 8, 2);
-            WTC_TILE(12, 384, 8, 1);
+            WTC_TILE(7, 384, 8, 1);
+            WTC_TILE(8, 512, 8, 2);
+            WTC_TILE(9, 512, 4, 1);
+            WTC_TILE(10, 512, 2, 1);
+            WTC_TILE(11, 64, 16, 1);
+            WTC_TILE(12, 128, 16, 1);
         }
     } else {
         constexpr int E = 4 / sizeof(T);  // twice the channels a unit, half the steps
@@ -312,7 +312,8 @@ int pick_tile(int64_t B, int64_t S, int C, double& best_score)
         const double tiles = flat ? (double)(B * S + pixels - 1) / pixels : (double)B * ((S + pixels - 1) / pixels);
         const double lanes = (double)C / ((C + step - 1) / step * step) * ((double)(B * S) / (tiles * pixels));
         const int run = pixels * (int)sizeof(T);
-        const double lines = run >= 128 ? 1.0 : run >= 64 ? 0.9 : 0.6;
+        // (shorter runs meet in the XCD's L2; off alignment each has two ends in lines of others)
+        const double lines = run >= 128 ? 1.0 : run >= 64 || REGULAR ? 0.9 : 0.7;
         const double score = lanes * lines * (tiles >= 512 ? 1.0 : tiles / 512);
         if (score > best_score) {
             best_score = score;
