@@ -1,5 +1,6 @@
 // Layer norm over the channels of each pixel, forward and backward: the
-// kernels for any number of channels, and which kernels run.
+// kernels for any number of channels, the sum of the workgroups' partial sums,
+// and which kernels run.
 #include "norm_device.h"
 
 namespace wtc {
@@ -35,7 +36,10 @@ DEV float weight(const NormArgs& a, int c) { return a.w ? a.w[c] : 1.0f; }
 DEV float bias(const NormArgs& a, int c) { return a.b ? a.b[c] : 0.0f; }
 
 // ----------------------------------------------------------------------------
-// any number of channels: the input is swept again for each statistic
+// any number of channels, and planes whose offsets pass 32 bits within a tile:
+// the input is swept again for each statistic (three and two sweeps from cache
+// for one from memory; 8 images of 1600 float32 channels, 49 x 49, took 460 and
+// 975 us, a third of the tiles' rate)
 // ----------------------------------------------------------------------------
 
 // One row a wavefront.
@@ -245,7 +249,8 @@ __global__ void __launch_bounds__(kThreads) planes_sums_any(const NormArgs a)
 }
 
 // The sums of the rows of partial sums, in a fixed order: 16 columns a
-// workgroup, every 16th row a thread, several rows on their way at once.
+// workgroup, every 16th row a thread, several rows on their way at once. 4 us,
+// bound by latency (1024 rows of 192 sums).
 constexpr int kColumns = 16, kRows = kThreads / kColumns;
 
 __global__ void __launch_bounds__(kThreads)

@@ -10,7 +10,18 @@
 // backward pass keeps the weight's and bias's gradients of its channels in
 // registers over all of its workgroup's tiles.
 //
-// Bound by memory.
+// Bound by memory where runs of pixels and units of channels are whole: 64
+// images of 96 channels, 56 x 56, float32, planes to rows, forward 31.7 us (4.9
+// TB/s of x and y), backward 46 us (5.0 TB/s of x, dy and dx; a large copy
+// reaches 5.3); 16 images of 64 channels, 224 x 224, planes to planes, 74.5 us
+// (5.5 TB/s) and 137 us (4.5). In 16 bits the forward pass still is (128 images,
+// bfloat16, 30.7 us, 5.0 TB/s); the backward pass waits at its barriers with the
+// three wavefronts a SIMD that its registers leave (82 us, 2.8 TB/s). Fewer
+// registers by force (128) made that 73 us and smaller planes slower (384
+// channels, 14 x 14: 21.7 to 25.9 us); x and dy kept as they are stored, 76 us,
+// and odd sizes slower (62 to 75 us). Odd channels and odd images cost 1.3 to
+// 1.9 times the regular ones (32 images of 95 channels, 63 x 95, bfloat16: 32
+// and 62 us, 2.3 and 1.8 TB/s).
 #pragma once
 
 #include "turn.h"
@@ -324,15 +335,19 @@ int pick_tile(int64_t B, int64_t S, int C, double& best_score)
 }
 
 // Calls f with the tile for these planes, false where there is none: vectors of
-// four pixels, but for images so small that most of them would be incomplete
-// (single pixels then run over all images).
+// four pixels, but for images so small that too many of them would be incomplete
+// (single pixels then run over all images). 128 channels, forward and backward,
+// single pixels against fours. float32, whose single pixels are slower: images of
+// 9 pixels 13.3 + 40.0 and 13.7 + 28.0 us (of the tiles' scores the ratio is 0.34),
+// of 3 12.9 + 29.3 and 15.9 + 32.1. bfloat16: of 35 9.7 + 25.8 and 11.4 + 29.1 (ratio
+// 0.61), of 81 11.0 + 32.5 and 11.3 + 28.8 (0.70).
 template <typename T, typename F>
 bool with_tile(int64_t B, int64_t S, int C, F&& f)
 {
     double fours = 0, ones = 0;
     if (S % 4 == 0 && C % (16 / (int)sizeof(T)) == 0) return planes_tile<T, 4, true>(pick_tile<T, 4, true>(B, S, C, fours), f);
     const int i = pick_tile<T, 4, false>(B, S, C, fours), j = pick_tile<T, 1, false>(B, S, C, ones);
-    return fours >= 0.5 * ones ? planes_tile<T, 4, false>(i, f) : planes_tile<T, 1, false>(j, f);
+    return fours >= (sizeof(T) == 4 ? 0.3 : 0.65) * ones ? planes_tile<T, 4, false>(i, f) : planes_tile<T, 1, false>(j, f);
 }
 
 // Workgroups of the backward pass: as many as are resident by the registers that

@@ -6,7 +6,11 @@
 // wavefront. WHOLE: C is a multiple of V; else the last vector is incomplete,
 // and rows may begin at any element.
 //
-// Bound by memory.
+// Bound by memory where many rows are on their way (191520 rows of 96 float32
+// channels: forward 34 us, 4.3 TB/s, backward 49 us, 4.5 TB/s); in 16 bits the
+// sums over lanes and the conversions show (the same rows in bfloat16 23.7 us,
+// 3.1 TB/s, and 37 us, 3.0 TB/s; 47880 rows of 127 float16 channels 10.6 and
+// 15.4 us, 2.3 TB/s).
 #include "norm_device.h"
 
 namespace wtc {
