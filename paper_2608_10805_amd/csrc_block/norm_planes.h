@@ -12,16 +12,13 @@
 //
 // Bound by memory where runs of pixels and units of channels are whole: 64
 // images of 96 channels, 56 x 56, float32, planes to rows, forward 31.7 us (4.9
-// TB/s of x and y), backward 46 us (5.0 TB/s of x, dy and dx; a large copy
-// reaches 5.3); 16 images of 64 channels, 224 x 224, planes to planes, 74.5 us
-// (5.5 TB/s) and 137 us (4.5). In 16 bits the forward pass still is (128 images,
-// bfloat16, 30.7 us, 5.0 TB/s); the backward pass waits at its barriers with the
-// three wavefronts a SIMD that its registers leave (82 us, 2.8 TB/s). Fewer
-// registers by force (128) made that 73 us and smaller planes slower (384
-// channels, 14 x 14: 21.7 to 25.9 us); x and dy kept as they are stored, 76 us,
-// and odd sizes slower (62 to 75 us). Odd channels and odd images cost 1.3 to
-// 1.9 times the regular ones (32 images of 95 channels, 63 x 95, bfloat16: 32
-// and 62 us, 2.3 and 1.8 TB/s).
+// TB/s of x and y), backward 41 to 45 us (5.1 to 5.6 TB/s of x, dy and dx; a large
+// copy reaches 5.3); 16 images of 64 channels, 224 x 224, planes to planes, 74.5 us
+// (5.5 TB/s) and 137 us (4.5). In 16 bits 128 images of 96 channels, 56 x 56, take
+// 31 us (5.0 TB/s) and 51 us (4.5), the backward pass with three wavefronts a SIMD
+// by its registers. Odd channels and odd images cost up to twice the regular ones
+// (32 images of 95 channels, 63 x 95, bfloat16: 32 and 61 us, 2.3 and 1.9 TB/s; of
+// 96 channels, 64 x 96: 18 and 31 us).
 #pragma once
 
 #include "turn.h"
@@ -149,7 +146,14 @@ __global__ void __launch_bounds__(Ti::TH) planes_forward(const NormArgs a, const
     }
 }
 
-template <typename Ti, bool OUT_PLANES>
+// DIRECT: dy's rows go from memory into LDS, the next tile's as soon as all have
+// read this one's, instead of through registers after x has come. Planes to rows
+// without and with it: bfloat16, 128 images of 96 channels, 56 x 56, 57.2 and 51.4
+// us, 64 of 768, 14 x 14, 36.3 and 30.8; float32, 64 of 96, 56 x 56, 49.2 and 45.2.
+// (x read ahead as well cost a wavefront a SIMD: 64 of 64 bfloat16 channels, 112 x
+// 112, with the last sums 72.4 and 87.0 us.) It needs rows that begin at multiples
+// of 16 bytes and units that are whole.
+template <typename Ti, bool OUT_PLANES, bool DIRECT>
 __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, const Pixels ps)
 {
     using T = typename Ti::Type;
@@ -161,6 +165,14 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
     const float per = 1.0f / a.C;
     float sw[K][G] = {}, sb[K][G] = {};
     const uint32_t first = !Ti::kShared || gridDim.x % 8 ? blockIdx.x : follow(blockIdx.x, gridDim.x);
+    const auto fetch = [&](uint32_t tile) ALWAYS {
+        if constexpr (DIRECT)
+            if (tile < ps.tiles) {
+                const uint32_t q0 = tile * Ti::P;
+                Tu::fetch((const T*)a.dy + q0 * a.dy_stride, a.dy_stride, turn, ps.N - q0, a.C / G);
+            }
+    };
+    fetch(first);
     for (uint32_t tile = first; tile < ps.tiles; tile += gridDim.x) {
         const Place<Ti> at(ps, tile, px, slot);
         float xhat[K][V][G], g[K][V][G], s1[V] = {}, s2[V] = {}, mean[V], rstd[V];
@@ -178,7 +190,13 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
             mean[i] = m.v[i];
             rstd[i] = r.v[i];
         }
-        if constexpr (!OUT_PLANES) {
+        if constexpr (DIRECT) {
+            Tu::fetched();
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (left[k] > 0) Tu::get(turn, px, k * NS + slot, g[k]);
+        } else if constexpr (!OUT_PLANES) {
 #pragma unroll
             for (int k0 = 0; k0 < K; k0 += Tu::kSteps) {
                 const int c0 = k0 * Ti::kChannels;
@@ -210,9 +228,14 @@ __global__ void __launch_bounds__(Ti::TH) planes_backward(const NormArgs a, cons
                     s2[i] += g[k][i][j] * xhat[k][i][j];
                 }
         }
-        if (!a.out) continue;
-        __syncthreads();  // the last tile's sums have been read
+        if (!a.out) {
+            if constexpr (DIRECT) __syncthreads();
+            fetch(tile + gridDim.x);
+            continue;
+        }
+        if constexpr (!DIRECT) __syncthreads();  // the last tile's sums have been read
         slot_sum<Ti>(s1, red[0]);
+        fetch(tile + gridDim.x);
         slot_sum<Ti>(s2, red[1]);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -386,9 +409,14 @@ bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t
         else if (forward)
             hipLaunchKernelGGL((planes_forward<Ti, false>), grid, block, 0, s, a, ps);
         else if (out_planes)
-            hipLaunchKernelGGL((planes_backward<Ti, true>), grid, block, 0, s, a, ps);
-        else
-            hipLaunchKernelGGL((planes_backward<Ti, false>), grid, block, 0, s, a, ps);
+            hipLaunchKernelGGL((planes_backward<Ti, true, false>), grid, block, 0, s, a, ps);
+        else if constexpr (Turn<Ti>::kDirect) {
+            if (((uintptr_t)a.dy | (uintptr_t)a.dy_stride * sizeof(T)) % 16 == 0)
+                hipLaunchKernelGGL((planes_backward<Ti, false, true>), grid, block, 0, s, a, ps);
+            else
+                hipLaunchKernelGGL((planes_backward<Ti, false, false>), grid, block, 0, s, a, ps);
+        } else
+            hipLaunchKernelGGL((planes_backward<Ti, false, false>), grid, block, 0, s, a, ps);
     });
     return done;
 }

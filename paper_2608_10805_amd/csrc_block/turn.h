@@ -121,6 +121,28 @@ struct Turn {
         if (!OUT && rows < Ti::P)
             for (int i = rows * U + threadIdx.x; i < Ti::P * U; i += Ti::TH) lds[i] = uint4{0, 0, 0, 0};
     }
+
+    // The rows' side from memory without registers between: `rows` rows (up to P)
+    // of `per` whole units, all addresses multiples of 16 bytes. What is not there
+    // stays as it was. Lane l of a wavefront writes the l-th unit of 64 adjacent
+    // ones, so that it is the lane that finds the unit that belongs there.
+    static constexpr bool kDirect = Ti::kRegular && kSteps == Ti::K;
+    static DEV void fetch(const T* mem, int64_t pitch, uint4* lds, uint32_t rows, int per)
+    {
+        static_assert(kSize % 64 == 0, "whole wavefronts");
+        const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int n = 0; n < (kSize + Ti::TH - 1) / Ti::TH; ++n) {
+            const int i0 = n * Ti::TH + w * 64;
+            if (kSize % Ti::TH && i0 >= kSize) break;
+            const int i = i0 + lane, r = i / U, u = turned(r / Ti::V, i % U);
+            if ((uint32_t)r < rows && u < per)
+                __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(mem + r * pitch + u * Ti::G),
+                                                 (__attribute__((address_space(3))) void*)(lds + i0), 16, 0, 0);
+        }
+    }
+    // Waits for this wavefront's part of it.
+    static DEV void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 };
 
 // The planes that tiles run over, and n / d for n < 2^31 as (n * magic) >> shift.

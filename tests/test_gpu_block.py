@@ -124,6 +124,31 @@ def test_norm_of_strided_rows(dtype, C, shift):
     assert torch.equal(wide, before)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B,C,S", [(3, 48, 64), (9, 96, 784), (40, 768, 196), (2, 128, 20)])
+@pytest.mark.parametrize("more,shift", [(0, 0), (16, 8), (5, 0), (8, 1)])
+def test_norm_of_planes_with_strided_gradient_rows(dtype, B, C, S, more, shift):
+    """dy as rows inside wider rows, aligned to 16 bytes or not; all of the gradients, and each by itself."""
+    x, dy, w, b = norm_problem("turned", B, C, S, dtype)
+    pitch = C + more
+    wide = torch.full((B * S * pitch + shift,), float("nan"), dtype=dy.dtype, device=DEV)[shift:].view(B, S, pitch)
+    up = wide[..., :C]
+    up.copy_(dy)
+    _, mean, rstd = binding.layer_norm_forward(x, w, b, 1e-6, 1, -1)
+    back = lambda t, **k: binding.layer_norm_backward(t, x, mean, rstd, w, 1e-6, 1, -1, **k)  # noqa: E731
+    dx, dw, db = back(up)
+    want = reference(x, dy, w, b, "turned", 1e-6)
+    sums = 8 * float(B * S) ** 0.5
+    ref.close(dx, want[1], dtype, 64 + C / 16, scale=float(dy.float().abs().max() * want[4].max() * w.abs().max()))
+    ref.close(dw, want[2], "f32", 64, sums + float(want[2].abs().max()))
+    ref.close(db, want[3], "f32", 64, sums + float(want[3].abs().max()))
+    # neither the rows' place nor which gradients are asked for changes a result
+    for a, o in zip(back(dy), (dx, dw, db)):
+        assert torch.equal(a, o)
+    assert torch.equal(back(up, need_dweight=False, need_dbias=False)[0], dx)
+    assert all(torch.equal(a, o) for a, o in zip(back(up, need_dx=False)[1:], (dw, db)))
+
+
 @pytest.mark.parametrize("layout", list(LAYOUTS))
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shift", [1, 2])
