@@ -11,6 +11,8 @@
 
 namespace wtc {
 
+constexpr int64_t kMaxThreads = (int64_t)1 << 32;  // threads of one launch stay below, along each dimension
+
 struct NormArgs {
     const void* x;
     const void* dy;
@@ -68,7 +70,7 @@ int64_t norm_parts(const wtconv_norm_desc& d);      // rows of partial sums of t
 int64_t residual_parts(const wtconv_residual_desc& d);
 
 // The kernels that hold every channel of a pixel in registers; false, with
-// nothing launched, where there are too many.
+// nothing launched, where there are too many, or more pixels than one launch takes.
 bool launch_rows_forward(wtconv_dtype dt, const NormArgs& a, hipStream_t s);
 bool launch_rows_backward(wtconv_dtype dt, const NormArgs& a, hipStream_t s);
 bool launch_planes_f32(bool forward, bool out_planes, const NormArgs& a, hipStream_t s);
@@ -81,6 +83,7 @@ hipError_t launch_norm_backward(const wtconv_norm_desc& d, NormArgs a, float* dw
 hipError_t launch_residual_forward(wtconv_dtype dt, const ResidualArgs& a, hipStream_t s);
 hipError_t launch_residual_backward(wtconv_dtype dt, ResidualArgs a, float* dgamma, hipStream_t s);
 int64_t adam_chunk_elements();
+int64_t adam_most_chunks();  // of one launch
 hipError_t launch_adamw(wtconv_dtype dt, int bits, const AdamArgs& a, hipStream_t s);
 hipError_t launch_adamw_moments(wtconv_dtype dt, int64_t n, const uint8_t* m, const uint8_t* ms, const uint8_t* v,
                                 const uint8_t* vs, void* om, void* ov, hipStream_t s);

@@ -348,6 +348,23 @@ hipError_t launch_norm_forward(const wtconv_norm_desc& d, const NormArgs& a, hip
 {
     if (d.in == WTCONV_ROWS ? launch_rows_forward(d.dtype, a, s) : launch_planes(true, d, a, s))
         return hipGetLastError();
+    // More pixels than one launch takes (at most 256 threads a pixel): in two halves.
+    const bool rows = d.in == WTCONV_ROWS;
+    if (a.N >= kMaxThreads / 256 && (rows || a.B > 1)) {
+        NormArgs half = a;
+        half.B = a.B / 2;  // (of no concern to rows)
+        half.N = rows ? a.N / 2 : half.B * a.S;
+        const hipError_t e = launch_norm_forward(d, half, s);
+        if (e != hipSuccess) return e;
+        const int64_t size = d.dtype == WTCONV_F32 ? 4 : 2;
+        half.x = (const char*)a.x + half.N * (rows ? a.x_stride : a.C) * size;
+        half.out = (char*)a.out + half.N * a.C * size;
+        half.mean = a.mean ? a.mean + half.N : nullptr;
+        half.rstd = a.rstd ? a.rstd + half.N : nullptr;
+        half.N = a.N - half.N;
+        half.B = a.B - half.B;
+        return launch_norm_forward(d, half, s);
+    }
     switch (d.dtype) {
         case WTCONV_F32: return forward_t<float>(d, a, s);
         case WTCONV_BF16: return forward_t<uint16_t>(d, a, s);

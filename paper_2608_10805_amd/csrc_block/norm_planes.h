@@ -402,6 +402,7 @@ bool planes_launch(bool forward, bool out_planes, const NormArgs& a, hipStream_t
         using Ti = decltype(t);
         Pixels ps;
         if (!pixels_of<Ti>(a.B, a.S, a.C, ps)) return;
+        if (forward && ((int64_t)ps.tiles + 7) / 8 * 8 * Ti::TH >= kMaxThreads) return;
         done = true;
         const dim3 grid(forward ? (ps.tiles + 7) / 8 * 8 : (unsigned)a.nparts), block(Ti::TH);
         if (forward && out_planes)

@@ -187,14 +187,16 @@ bool layout(int n, bool forward, int& gl, int& r)
 }
 
 template <typename T, int R, bool WHOLE>
-void launch_r(bool forward, const NormArgs& a, int gl, hipStream_t s)
+bool launch_r(bool forward, const NormArgs& a, int gl, hipStream_t s)
 {
     const int groups = kThreads / gl;
+    if (forward && (a.N + groups - 1) / groups * kThreads >= kMaxThreads) return false;
     if (forward)
         hipLaunchKernelGGL((rows_forward<T, R, WHOLE>), dim3((unsigned)((a.N + groups - 1) / groups)), dim3(kThreads),
                            0, s, a, gl);
     else
         hipLaunchKernelGGL((rows_backward<T, R, WHOLE>), dim3(a.nparts), dim3(kThreads), (size_t)a.C * 8, s, a, gl);
+    return true;
 }
 
 template <typename T, bool WHOLE>
@@ -204,11 +206,11 @@ bool launch_v(bool forward, const NormArgs& a, hipStream_t s)
     int gl = 0, r = 0;
     if (!layout((a.C + V - 1) / V, forward, gl, r)) return false;
     switch (r) {
-        case 1: launch_r<T, 1, WHOLE>(forward, a, gl, s); return true;
-        case 2: launch_r<T, 2, WHOLE>(forward, a, gl, s); return true;
-        case 3: launch_r<T, 3, WHOLE>(forward, a, gl, s); return true;
-        case 4: launch_r<T, 4, WHOLE>(forward, a, gl, s); return true;
-        case 8: launch_r<T, 8, WHOLE>(forward, a, gl, s); return true;
+        case 1: return launch_r<T, 1, WHOLE>(forward, a, gl, s);
+        case 2: return launch_r<T, 2, WHOLE>(forward, a, gl, s);
+        case 3: return launch_r<T, 3, WHOLE>(forward, a, gl, s);
+        case 4: return launch_r<T, 4, WHOLE>(forward, a, gl, s);
+        case 8: return launch_r<T, 8, WHOLE>(forward, a, gl, s);
     }
     return false;
 }
@@ -221,7 +223,6 @@ bool launch_t(bool forward, const NormArgs& a, hipStream_t s)
 
 bool launch(wtconv_dtype dt, bool forward, const NormArgs& a, hipStream_t s)
 {
-    if (a.N > (int64_t)1 << 30) return false;  // workgroups of one launch
     switch (dt) {
         case WTCONV_F32: return launch_t<float>(forward, a, s);
         case WTCONV_BF16: return launch_t<uint16_t>(forward, a, s);

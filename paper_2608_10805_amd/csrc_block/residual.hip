@@ -26,7 +26,7 @@ DEV float wave_sum(float v)
 }
 
 // ----------------------------------------------------------------------------
-// tensors whose offsets pass 32 bits within a tile
+// tensors whose offsets pass 32 bits within a tile, or with more tiles than one launch takes
 // ----------------------------------------------------------------------------
 
 // Workgroup: 64 channels (blockIdx.y), one tile of 64 pixels after another.
@@ -225,6 +225,7 @@ bool launch(bool forward, const ResidualArgs& a, hipStream_t s)
 {
     Pixels ps;
     if (!pixels_of<Ti>(a.B, a.S, a.C, ps)) return false;
+    if (forward && ((int64_t)ps.tiles + 7) / 8 * 8 * Ti::TH >= kMaxThreads) return false;
     const unsigned blocks = (unsigned)((a.C + Ti::kMaxC - 1) / Ti::kMaxC);
     if (forward)
         hipLaunchKernelGGL(residual_forward<Ti>, dim3((ps.tiles + 7) / 8 * 8, blocks), dim3(Ti::TH), 0, s, a, ps);

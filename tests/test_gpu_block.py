@@ -293,6 +293,53 @@ def test_norm_beyond_32_bits_of_elements():
     ref.close(z[-1, :, -2:].T, want, "bf16", 64 + 65536 / 16)
 
 
+@pytest.mark.parametrize("layout", ["turned", "planes"])
+def test_norm_of_more_pixels_than_one_launch_takes(layout):
+    """2^30 images of one pixel: 2^32 threads. Every pixel against the two values that a norm of two channels has."""
+    n = (1 << 30) + 67
+    x = torch.zeros(n, 2, 1, dtype=torch.float16, device=DEV)
+    x[:, 0] = 1.0
+    x[1::2, 0] = -3.0
+    w, b = torch.tensor([1.0, 2.0], device=DEV), torch.tensor([0.5, -0.5], device=DEV)
+    y, mean, rstd = binding.layer_norm_forward(x, w, b, 0.0, *LAYOUTS[layout])
+    del x
+    assert bool((mean[::2] == 0.5).all()) and bool((mean[1::2] == -1.5).all())
+    for part, r in ((rstd[::2], 2.0), (rstd[1::2], 2 / 3)):  # to two roundings
+        assert float((part - r).abs().max()) <= r * 2.0 ** -22
+    del mean, rstd, part
+    # xhat = 1 and -1, then -1 and 1; to two roundings of the result (at most 2.5)
+    for part, want in ((y[::2], (1.5, -2.5)), (y[1::2], (-0.5, 1.5))):
+        for c in (0, 1):
+            v = part.reshape(part.shape[0], 2)[:, c]
+            assert float(v.max()) - 2.0 ** -9 <= want[c] <= float(v.min()) + 2.0 ** -9
+    torch.cuda.empty_cache()
+
+
+def test_norm_of_more_rows_than_one_launch_takes():
+    """2^30 rows of four lanes each: 2^32 threads. Rows of another kind lie at both ends and around the middle."""
+    if torch.cuda.mem_get_info()[0] < 150e9:
+        pytest.skip("needs 125 GB of GPU memory")
+    n, C = (1 << 30) + 5, 25
+    x = torch.zeros(n, C, dtype=torch.float16, device=DEV)
+    places = [0, 1, n // 4, n // 2 - 1, n // 2, n // 2 + 1, 3 * (n // 4), n - 2, n - 1]
+    some = normal(gen(12), (len(places), C), "f16")
+    for p, row in zip(places, some):
+        x[p].copy_(row)
+    want = ref.norm(some.double().cpu(), None, None, 1e-6)
+    y, mean, rstd = binding.layer_norm_forward(x, None, None, 1e-6)
+    del x
+    ref.close(torch.stack([y[p] for p in places]), want[0], "f16", 64)
+    ref.close(torch.stack([rstd[p] for p in places]), want[2].view(-1), "f32", 64)
+    assert int(mean.count_nonzero()) == len(places)
+    others = torch.ones(n, dtype=torch.bool, device=DEV)
+    others[places] = False
+    for i in range(0, n, 1 << 26):
+        part = y[i:i + (1 << 26)]
+        assert not bool((part != 0).any(1).logical_and_(others[i:i + (1 << 26)]).any())
+    del y, part
+    torch.cuda.empty_cache()
+
+
 def test_norm_in_a_graph():
     """A captured forward and backward, replayed with the program's own work between, gives the eager bits."""
     x, dy, w, b = norm_problem("turned", 4, 96, (14, 14), "f32")
