@@ -212,6 +212,7 @@ hipError_t moments_t(int64_t n, const uint8_t* m, const uint8_t* ms, const uint8
 }  // namespace
 
 int64_t adam_chunk_elements() { return kChunk; }
+int64_t adam_most_chunks() { return kMaxThreads / kThreads - 1; }
 
 hipError_t launch_adamw(wtconv_dtype dt, int bits, const AdamArgs& a, hipStream_t s)
 {

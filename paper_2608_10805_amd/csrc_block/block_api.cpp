@@ -9,7 +9,6 @@
 namespace wtc {
 namespace {
 
-constexpr int64_t kMaxChunks = (int64_t)1 << 30;    // workgroups of one launch
 constexpr int64_t kMaxElements = (int64_t)1 << 46;  // far below where byte offsets pass 63 bits
 
 size_t element_size(wtconv_dtype dt) { return dt == WTCONV_F32 ? 4 : 2; }
@@ -252,10 +251,10 @@ wtconv_status wtconv_adamw_step(int n_groups, const wtconv_adamw_group* groups, 
         if (misaligned(g.exp_avg, 16) || misaligned(g.exp_avg_sq, 16)) return WTCONV_ERR_SHAPE;
     }
     const size_t e = element_size(dtype);
-    const int64_t chunk = adam_chunk_elements();
+    const int64_t chunk = adam_chunk_elements(), most = adam_most_chunks();
     for (int i = 0; i < n_tensors; ++i) {
         const wtconv_adamw_tensor& t = tensors[i];
-        if (t.numel < 0 || t.numel / chunk >= kMaxChunks || t.offset < 0 || t.offset > kMaxElements || t.offset % 64 ||
+        if (t.numel < 0 || t.numel > kMaxElements || t.offset < 0 || t.offset > kMaxElements || t.offset % 64 ||
             t.group < 0 || t.group >= n_groups)
             return WTCONV_ERR_SHAPE;
         if (!t.numel) continue;
@@ -279,40 +278,44 @@ wtconv_status wtconv_adamw_step(int n_groups, const wtconv_adamw_group* groups, 
     for (int i = 0; i < n_tensors; ++i) {
         const wtconv_adamw_tensor& t = tensors[i];
         if (!t.numel) continue;
-        const int64_t chunks = (t.numel + chunk - 1) / chunk;
-        int place = 0;
-        while (place < places && loaded[place] != t.group) ++place;
-        if (a.count == kAdamTensors || place == kAdamGroups || a.chunks + chunks >= kMaxChunks) {
-            const hipError_t err = flush();
-            if (err != hipSuccess) return WTCONV_ERR_HIP;
-            place = 0;
+        // (a tensor of more chunks than one launch takes goes in pieces of whole chunks)
+        for (int64_t done = 0; done < t.numel; done += most * chunk) {
+            const int64_t numel = t.numel - done < most * chunk ? t.numel - done : most * chunk;
+            const int64_t chunks = (numel + chunk - 1) / chunk;
+            int place = 0;
+            while (place < places && loaded[place] != t.group) ++place;
+            if (a.count == kAdamTensors || place == kAdamGroups || a.chunks + chunks > most) {
+                const hipError_t err = flush();
+                if (err != hipSuccess) return WTCONV_ERR_HIP;
+                place = 0;
+            }
+            if (place == places) {
+                const wtconv_adamw_group& g = groups[t.group];
+                AdamGroup& o = a.group[place];
+                o.m = g.exp_avg;
+                o.v = g.exp_avg_sq;
+                o.ms = g.exp_avg_scale;
+                o.vs = g.exp_avg_sq_scale;
+                o.b1 = (float)g.beta1;
+                o.omb1 = (float)(1 - g.beta1);
+                o.b2 = (float)g.beta2;
+                o.omb2 = (float)(1 - g.beta2);
+                o.rcorr2 = (float)(1 / std::sqrt(1 - std::pow(g.beta2, (double)g.step)));
+                o.eps = (float)g.eps;
+                o.keep = (float)(1 - g.lr * g.weight_decay);
+                o.rate = (float)(g.lr / (1 - std::pow(g.beta1, (double)g.step)));
+                o.key = g.key;
+                loaded[places++] = t.group;
+            }
+            a.p[a.count] = (char*)t.param + done * e;
+            a.g[a.count] = (const char*)t.grad + done * e;
+            a.n[a.count] = numel;
+            a.at[a.count] = t.offset + done;
+            a.first[a.count] = a.chunks;
+            a.of[a.count] = (uint8_t)place;
+            a.chunks += (uint32_t)chunks;
+            ++a.count;
         }
-        if (place == places) {
-            const wtconv_adamw_group& g = groups[t.group];
-            AdamGroup& o = a.group[place];
-            o.m = g.exp_avg;
-            o.v = g.exp_avg_sq;
-            o.ms = g.exp_avg_scale;
-            o.vs = g.exp_avg_sq_scale;
-            o.b1 = (float)g.beta1;
-            o.omb1 = (float)(1 - g.beta1);
-            o.b2 = (float)g.beta2;
-            o.omb2 = (float)(1 - g.beta2);
-            o.rcorr2 = (float)(1 / std::sqrt(1 - std::pow(g.beta2, (double)g.step)));
-            o.eps = (float)g.eps;
-            o.keep = (float)(1 - g.lr * g.weight_decay);
-            o.rate = (float)(g.lr / (1 - std::pow(g.beta1, (double)g.step)));
-            o.key = g.key;
-            loaded[places++] = t.group;
-        }
-        a.p[a.count] = t.param;
-        a.g[a.count] = t.grad;
-        a.n[a.count] = t.numel;
-        a.at[a.count] = t.offset;
-        a.first[a.count] = a.chunks;
-        a.of[a.count] = (uint8_t)place;
-        a.chunks += (uint32_t)chunks;
-        ++a.count;
     }
     return of(flush());
 }
