@@ -2,9 +2,10 @@
 // every input, one write of every output. Bound by memory: 128 images of 96
 // bfloat16 channels, 56 x 56, 48 us forward (4.8 TB/s of x, z and y) and 59 us
 // backward with d_gamma's sums (3.9); 64 images of 192 float32 channels, 28 x
-// 28, 30 and 28 us (3.9 and 4.1 TB/s), of which the one round of workgroups that
-// such a tensor makes spends a fifth with loads or stores alone; 32 images of
-// 128 bfloat16 channels, 63 x 95 off alignment, 36 and 45 us (4.1 and 3.3 TB/s).
+// 28, 26 to 30 and 27 us (3.9 to 4.4 and 4.3 TB/s), of which the one round of
+// workgroups that such a tensor makes spends a fifth with loads or stores alone;
+// 32 images of 128 bfloat16 channels, 63 x 95 off alignment, 33 to 37 and 44 us
+// (4.0 to 4.4 and 3.4 TB/s).
 //
 // A workgroup takes tiles of P pixels by a block of channels; rows are turned in
 // LDS (turn.h), where a thread's own units are its own on both ways, so that z
