@@ -142,8 +142,23 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamArgs a)
                 m[i] = m[i] * h.b1 + gr * h.omb1;
                 v[i] = v[i] * h.b2 + gr * gr * h.omb2;
             }
-            // square root and reciprocal to one unit in the last place: the update is far below the parameter
-            const float denom = __builtin_amdgcn_sqrtf(v[i]) * h.rcorr2 + h.eps;
+        }
+        // square root and reciprocal to one unit in the last place: the update is far below the parameter
+        float root[kVec];
+        // the hardware's root of a subnormal is zero; what it should be, up to 2^-63, is less than a rounding beside
+        // all but the smallest eps
+        if (h.eps < 0x1p-38f * h.rcorr2) {
+            asm volatile("");  // (keeps this a branch: else both sides are computed)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                root[i] = v[i] < 0x1p-96f ? __builtin_amdgcn_sqrtf(v[i] * 0x1p64f) * 0x1p-32f : __builtin_amdgcn_sqrtf(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) root[i] = __builtin_amdgcn_sqrtf(v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float denom = root[i] * h.rcorr2 + h.eps;
             pp.v[i] = from_f32<T>(to_f32(pp.v[i]) * h.keep - m[i] * __builtin_amdgcn_rcpf(denom) * h.rate);
         }
         store_upto<kVec>(at_bytes(p, c * sizeof(T)), left, pp);

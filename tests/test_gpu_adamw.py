@@ -165,6 +165,21 @@ def test_non_finite_gradients(bits, bad):
     assert torch.equal(ps[0].detach()[other], good[0].detach()[other])
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -80])
+def test_second_moments_below_the_normal_numbers(bits, eps):
+    """Gradients whose squares are subnormal, with an eps that does not hide them. Every moment is a power of two,
+    which float32 holds exactly."""
+    for power in (-55, -60, -64, -68):  # v = 2^-120, 2^-130, 2^-138, 2^-146
+        p = torch.nn.Parameter(torch.ones(200, device=DEV))
+        p.grad = torch.full((200,), 2.0 ** power, device=DEV)
+        optim.AdamW([p], lr=0.125, betas=(0.5, 1 - 2.0 ** -10), eps=eps, weight_decay=0.0, state_bits=bits).step()
+        zero = torch.zeros(1, dtype=torch.float64)
+        want, _, _ = ref.adamw(torch.ones(200, dtype=torch.float64), d(p.grad), zero, zero, 1, 0.125,
+                               (0.5, 1 - 2.0 ** -10), eps, 0.0)
+        ref.close(p, want, "f32", 8)
+
+
 def test_zero_gradients_and_a_zero_eps():
     p = torch.nn.Parameter(torch.ones(100, device=DEV))
     p.grad = torch.zeros(100, device=DEV)
