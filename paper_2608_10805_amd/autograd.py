@@ -129,6 +129,26 @@ def load_block(x):
     return _block
 
 
+class _Made(torch.autograd.Function):
+    """A gradient as a result of what it was made of, so that a gradient of it reaches this error."""
+
+    @staticmethod
+    def forward(ctx, grad, *sources):
+        return grad.detach()
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("the operators around the convolution cannot be differentiated twice")
+
+
+def _made_of(grad, *sources):
+    """A gradient that a backward pass was asked for, or None: with create_graph it depends on its sources (tensors or
+    None) that need gradients, and differentiating it is refused rather than taken for zero."""
+    if grad is None or not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in sources):
+        return grad
+    return _Made.apply(grad, *sources)
+
+
 def _dense_rows(t):
     return t if binding._row_stride(t) is not None else t.contiguous()
 
@@ -148,11 +168,12 @@ class LayerNormFunction(torch.autograd.Function):
         return (*_norm_backward((*ctx.args, *ctx.needs_input_grad[:3]), dy, *ctx.saved_tensors), None, None, None)
 
 
-@torch.autograd.function.once_differentiable
 def _norm_backward(args, dy, x, mean, rstd, weight):
     """args: eps, the two channel dimensions and which gradients are asked for."""
-    dy = _dense_rows(dy) if args[2] == -1 else dy.contiguous()
-    return binding.layer_norm_backward(dy, x, mean, rstd, weight, *args)
+    with torch.no_grad():
+        rows = _dense_rows(dy) if args[2] == -1 else dy.contiguous()
+        dx, dweight, dbias = binding.layer_norm_backward(rows, x, mean, rstd, weight, *args)
+    return _made_of(dx, dy, x, weight), _made_of(dweight, dy, x), _made_of(dbias, dy)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-6, channel_dim=-1, out_channel_dim=None):
@@ -196,12 +217,11 @@ class ScaledResidualFunction(torch.autograd.Function):
         return (*_residual_backward(ctx.needs_input_grad[:3], dy, *ctx.saved_tensors), None)
 
 
-@torch.autograd.function.once_differentiable
 def _residual_backward(need, dy, z, gamma, sample_scale):
     """need: which of the gradients of x, z and gamma are asked for."""
-    dy = dy.contiguous()
-    dz, dgamma = binding.scaled_residual_backward(dy, z, gamma, sample_scale, *need[1:])
-    return dy if need[0] else None, dz, dgamma
+    with torch.no_grad():
+        dz, dgamma = binding.scaled_residual_backward(dy.contiguous(), z, gamma, sample_scale, *need[1:])
+    return dy if need[0] else None, _made_of(dz, dy, gamma), _made_of(dgamma, dy, z)
 
 
 def scaled_residual(x, z, gamma=None, sample_scale=None):

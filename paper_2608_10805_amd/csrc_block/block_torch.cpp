@@ -145,9 +145,13 @@ variable_list from_python(PyObject* fn, py::tuple args)
     }
 }
 
-// Whether a backward has to go through Python: gradients of gradients are
-// refused there.
-bool twice(const Tensor& dy) { return at::GradMode::is_enabled() && dy.requires_grad(); }
+// Whether a backward has to go through Python: its gradients will be
+// differentiated, which is refused there. They depend on dy and on every saved
+// tensor that trains.
+bool twice(const Tensor& dy, const OptTensor& a, const OptTensor& b)
+{
+    return at::GradMode::is_enabled() && (dy.requires_grad() || (a && a->requires_grad()) || (b && b->requires_grad()));
+}
 
 // ----------------------------------------------------------------------------
 // layer norm
@@ -235,7 +239,7 @@ struct NormNode : public Node {
         const bool need_dx = task_should_compute_output(0), need_dw = task_should_compute_output(1),
                    need_db = task_should_compute_output(2);
         wtconv_norm_desc d;
-        const bool ok = !twice(dy) && describe(x, args, d) && plain(stats, x.device()) && stats.is_contiguous() &&
+        const bool ok = !twice(dy, x, w) && describe(x, args, d) && plain(stats, x.device()) && stats.is_contiguous() &&
                         stats.scalar_type() == at::kFloat && stats.numel() == 2 * d.B * d.S &&
                         vector_of(w, x.device(), d.C) && plain(dy, x.device()) &&
                         dy.scalar_type() == x.scalar_type() && dy.sizes() == at::IntArrayRef(out_sizes(x, args));
@@ -377,7 +381,7 @@ struct ResidualNode : public Node {
         if (has_keep) keep = keep_.unpack();
         const bool need_dx = task_should_compute_output(0), need_dz = task_should_compute_output(1),
                    need_dg = z && task_should_compute_output(2);
-        const bool second = twice(grads[0]);
+        const bool second = twice(grads[0], z, gamma);
         const Tensor dy = second ? grads[0] : grads[0].contiguous();
         wtconv_residual_desc d;
         if (!second && describe(dy, d) && vector_of(gamma, dy.device(), d.C) && vector_of(keep, dy.device(), d.B) &&
