@@ -449,14 +449,26 @@ py::object scaled_residual(py::handle x, py::handle z, py::handle gamma, py::han
 // What stays the same of a parameter group from step to step.
 struct Group {
     std::vector<int64_t> offsets, numel;
-    Tensor steps, m, v;  // steps: int64 on the host
+    std::vector<std::vector<int64_t>> orders;  // of the parameters' memory, as optim._order() has them
+    Tensor steps, m, v;                        // steps: int64 on the host
     OptTensor ms, vs;
 
-    Group(std::vector<int64_t> offsets_, std::vector<int64_t> numel_, Tensor steps_, Tensor m_, Tensor v_,
-          OptTensor ms_, OptTensor vs_)
-        : offsets(std::move(offsets_)), numel(std::move(numel_)), steps(std::move(steps_)), m(std::move(m_)),
-          v(std::move(v_)), ms(std::move(ms_)), vs(std::move(vs_))
+    Group(std::vector<int64_t> offsets_, std::vector<int64_t> numel_, std::vector<std::vector<int64_t>> orders_,
+          Tensor steps_, Tensor m_, Tensor v_, OptTensor ms_, OptTensor vs_)
+        : offsets(std::move(offsets_)), numel(std::move(numel_)), orders(std::move(orders_)),
+          steps(std::move(steps_)), m(std::move(m_)), v(std::move(v_)), ms(std::move(ms_)), vs(std::move(vs_))
     {
+    }
+
+    // Whether parameter i still lies in memory as its moments do.
+    bool in_order(size_t i, const Tensor& p) const
+    {
+        const std::vector<int64_t>& order = orders[i];
+        if (order.empty()) return p.is_contiguous();
+        if (order.size() != (size_t)p.dim() || p.is_contiguous()) return false;
+        for (size_t d = 0; d < order.size(); ++d)
+            if (order[d] != (p.size((int64_t)d) > 1 ? p.stride((int64_t)d) : 0)) return false;
+        return true;
     }
 };
 
@@ -503,7 +515,7 @@ bool adamw_step(const std::vector<Group*>& plans, py::sequence params, const std
             wtconv_dtype type;
             if (!plain(p, q.m.device(), false) || !plain(g, q.m.device(), false) || !type_of(p, type) ||
                 g.scalar_type() != p.scalar_type() || p.numel() != q.numel[i] || g.sizes() != p.sizes() ||
-                g.strides() != p.strides() || !p.is_non_overlapping_and_dense() || p.is_inference())
+                g.strides() != p.strides() || !q.in_order(i, p) || p.is_inference())
                 return false;
             if (dev && *dev != p.device()) return false;
             dev = p.device();
@@ -593,7 +605,8 @@ void init(const std::vector<uintptr_t>& fns, py::object norm_py, py::object resi
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
 {
     py::class_<Group>(m, "AdamWGroup")
-        .def(py::init<std::vector<int64_t>, std::vector<int64_t>, Tensor, Tensor, Tensor, OptTensor, OptTensor>());
+        .def(py::init<std::vector<int64_t>, std::vector<int64_t>, std::vector<std::vector<int64_t>>, Tensor, Tensor,
+                      Tensor, OptTensor, OptTensor>());
     m.def("init", &init);
     m.def("layer_norm", &layer_norm);
     m.def("scaled_residual", &scaled_residual);

@@ -30,6 +30,12 @@ def _strides_fill(t):
         (t.dim() == 5 and t.is_contiguous(memory_format=torch.channels_last_3d))
 
 
+def _order(t):
+    """The order of a dense tensor's memory: () for that of its shape, else its strides (0 for a dimension of one
+    element, whose stride says nothing)."""
+    return () if t.is_contiguous() else tuple(stride if n > 1 else 0 for n, stride in zip(t.shape, t.stride()))
+
+
 class AdamW(torch.optim.Optimizer):
     """AdamW (decoupled weight decay) on GPU parameters in float32, bfloat16 or float16:
 
@@ -42,16 +48,19 @@ class AdamW(torch.optim.Optimizer):
     repeated gives the same bits. A block of 64 that meets a value that is not finite stands for NaN from then on, as
     a 32-bit moment does.
 
-    The moments are allocated with the group. `state[p]` holds views of them: "exp_avg" and "exp_avg_sq" (shaped as p
-    with 32 bits; the codes, one a element in the order of memory, with 8), "exp_avg_scale" and "exp_avg_sq_scale" (8
-    bits), and "step", the number of steps p has taken. A parameter without a gradient is left alone.
+    The moments are allocated with the group, in the order of the parameters' memory. `state[p]` holds views of them:
+    "exp_avg" and "exp_avg_sq" (shaped as p with 32 bits; the codes, one an element in the order of memory, with 8),
+    "exp_avg_scale", "exp_avg_sq_scale" and "order" (8 bits: which order that is, () or the strides), and "step", the
+    number of steps p has taken. A parameter without a gradient is left alone. Where a parameter's memory gets another
+    order (to channels_last, say), moments in 32 bits follow it; those in 8 bits share their scales in the old order,
+    so that a step is refused unless it is the first.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, seed=0):
         if state_bits not in (8, 32):
             raise ValueError(f"state_bits must be 8 or 32, got {state_bits}")
         self.state_bits, self.seed = state_bits, int(seed)
-        self._buffers = []  # of each group: exp_avg, exp_avg_sq, their scales (8 bits), step, offsets, numel
+        self._buffers = []  # of each group: exp_avg, exp_avg_sq, their scales (8 bits), step, offsets, numel, orders
         self._native = []   # the same for the native host path
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
 
@@ -91,21 +100,45 @@ class AdamW(torch.optim.Optimizer):
         if coded:
             buffers.update(exp_avg_scale=new(end // block), exp_avg_sq_scale=new(end // block))
         buffers.update(step=torch.zeros(len(params), dtype=torch.int64), offsets=offsets,
-                       numel=[p.numel() for p in params])
+                       numel=[p.numel() for p in params], orders=[_order(p) for p in params])
         self._buffers.append(buffers)
+        self._native.append(self._plan(params, buffers))
+        for i, p in enumerate(params):
+            self._show(buffers, i, p)
+
+    def _plan(self, params, buffers):
+        """The group for the native host path, or None."""
         ext = autograd.load_block(params[0]) if params else False
-        self._native.append(ext.AdamWGroup(offsets, buffers["numel"], buffers["step"],
-                                           *(buffers.get(n) for n in ("exp_avg", "exp_avg_sq", "exp_avg_scale",
-                                                                      "exp_avg_sq_scale"))) if ext else None)
-        for i, (p, at) in enumerate(zip(params, offsets)):
-            n, state = p.numel(), {"step": buffers["step"][i]}
-            for name in ("exp_avg", "exp_avg_sq"):
-                if coded:
-                    state[name] = buffers[name][at:at + n]
-                    state[name + "_scale"] = buffers[name + "_scale"][at // block:at // block - (-n // block)]
-                else:
-                    state[name] = buffers[name][at:at + n].as_strided(p.shape, p.stride())
-            self.state[p] = state
+        return ext.AdamWGroup(*(buffers[n] for n in ("offsets", "numel", "orders", "step", "exp_avg", "exp_avg_sq")),
+                              *(buffers.get(n) for n in ("exp_avg_scale", "exp_avg_sq_scale"))) if ext else None
+
+    def _show(self, buffers, i, p):
+        """state[p] as views of the group's buffers, in the present order of p's memory."""
+        block, at, n = binding.ADAMW_BLOCK, buffers["offsets"][i], p.numel()
+        buffers["orders"][i] = _order(p)
+        self.state[p] = state = {"step": buffers["step"][i]}
+        for name in ("exp_avg", "exp_avg_sq"):
+            if self.state_bits == 8:
+                state[name] = buffers[name][at:at + n]
+                state[name + "_scale"] = buffers[name + "_scale"][at // block:at // block - (-n // block)]
+                state["order"] = buffers["orders"][i]
+            else:
+                state[name] = buffers[name][at:at + n].as_strided(p.shape, p.stride())
+
+    def _reorder(self, index, i, p):
+        """Bring the moments of a parameter whose memory has another order than they have into that order."""
+        buffers, held = self._buffers[index], self.state[p]
+        if self.state_bits == 32 and held["exp_avg"].shape == p.shape:
+            held = {name: held[name].clone() for name in ("exp_avg", "exp_avg_sq")}
+        elif int(held["step"]):
+            raise ValueError(f"a parameter of shape {tuple(p.shape)} changed its order of memory: its moments are in "
+                             "the old one")
+        else:  # there are none yet
+            held = {}
+        self._show(buffers, i, p)
+        for name, moment in held.items():
+            self.state[p][name].copy_(moment)
+        self._native[index] = self._plan(self.param_groups[index]["params"], buffers)
 
     def step(self, closure=None, grad_scale=None):
         """One step. grad_scale: a float32 GPU tensor of one element that every gradient is multiplied with (to undo
@@ -137,6 +170,8 @@ class AdamW(torch.optim.Optimizer):
                 if p.grad is None:
                     continue
                 grad = _gradient(p, buffers, i)
+                if _order(p) != buffers["orders"][i]:
+                    self._reorder(index, i, p)
                 device, step = p.device, steps[i] + 1
                 code = binding._dtype_code(p)
                 groups, tensors = calls.setdefault(code, ([], []))
@@ -185,16 +220,25 @@ class AdamW(torch.optim.Optimizer):
         saved, groups = state_dict["state"], state_dict["param_groups"]
         if [len(g["params"]) for g in groups] != [len(g["params"]) for g in self.param_groups]:
             raise ValueError("the state has other parameter groups")
-        pairs = [(p, saved[i]) for ours, g in zip(self.param_groups, groups) for p, i in zip(ours["params"], g["params"])
-                 if i in saved]
-        for p, state in pairs:
-            ours = self.state[p]
+        places = [(index, i, p, saved[j]) for index, (ours, g) in enumerate(zip(self.param_groups, groups))
+                  for i, (p, j) in enumerate(zip(ours["params"], g["params"])) if j in saved]
+        for _, _, p, state in places:
+            # (a state without "order" is a dense parameter's)
+            ours, state = {**self.state[p]}, {**state}
+            if tuple(state.pop("order", ())) != (_order(p) if ours.pop("order", None) is not None else ()):
+                raise ValueError(f"the 8-bit state is of a parameter in another order of memory than this one of shape "
+                                 f"{tuple(p.shape)}")
             if set(state) != set(ours) or any(state[k].shape != ours[k].shape or state[k].dtype != ours[k].dtype
                                               for k in ours):
                 raise ValueError("the state is not of these parameters, or was held in other bits")
-        for p, state in pairs:
+        for index, i, p, state in places:
+            buffers = self._buffers[index]
+            if _order(p) != buffers["orders"][i]:
+                self._show(buffers, i, p)
+                self._native[index] = self._plan(self.param_groups[index]["params"], buffers)
             for k, t in self.state[p].items():
-                t.copy_(state[k])
+                if k != "order":
+                    t.copy_(state[k])
         for ours, g in zip(self.param_groups, groups):
             ours.update({k: v for k, v in g.items() if k != "params"})
 
@@ -206,7 +250,8 @@ def _gradient(p, buffers, i):
         raise ValueError("AdamW takes dense gradients only")
     if p.numel() != buffers["numel"][i] or p.dtype not in _DTYPES or p.device != buffers["exp_avg"].device or \
             not _strides_fill(p):
-        raise ValueError(f"a parameter of shape {tuple(p.shape)} changed its size, type, device or order of memory")
+        raise ValueError(f"a parameter of shape {tuple(p.shape)} changed its size, type or device, or does not fill its "
+                         "memory any more")
     if grad.dtype != p.dtype or grad.device != p.device:
         raise ValueError(f"a gradient is {grad.dtype} on {grad.device}, its parameter {p.dtype} on {p.device}")
     if grad.stride() != p.stride() or not _strides_fill(grad):
