@@ -448,15 +448,17 @@ py::object scaled_residual(py::handle x, py::handle z, py::handle gamma, py::han
 
 // What stays the same of a parameter group from step to step.
 struct Group {
+    std::vector<Tensor> params;
     std::vector<int64_t> offsets, numel;
     std::vector<std::vector<int64_t>> orders;  // of the parameters' memory, as optim._order() has them
     Tensor steps, m, v;                        // steps: int64 on the host
     OptTensor ms, vs;
 
-    Group(std::vector<int64_t> offsets_, std::vector<int64_t> numel_, std::vector<std::vector<int64_t>> orders_,
-          Tensor steps_, Tensor m_, Tensor v_, OptTensor ms_, OptTensor vs_)
-        : offsets(std::move(offsets_)), numel(std::move(numel_)), orders(std::move(orders_)),
-          steps(std::move(steps_)), m(std::move(m_)), v(std::move(v_)), ms(std::move(ms_)), vs(std::move(vs_))
+    Group(std::vector<Tensor> params_, std::vector<int64_t> offsets_, std::vector<int64_t> numel_,
+          std::vector<std::vector<int64_t>> orders_, Tensor steps_, Tensor m_, Tensor v_, OptTensor ms_, OptTensor vs_)
+        : params(std::move(params_)), offsets(std::move(offsets_)), numel(std::move(numel_)),
+          orders(std::move(orders_)), steps(std::move(steps_)), m(std::move(m_)), v(std::move(v_)),
+          ms(std::move(ms_)), vs(std::move(vs_))
     {
     }
 
@@ -510,6 +512,7 @@ bool adamw_step(const std::vector<Group*>& plans, py::sequence params, const std
             const py::handle h = PyList_GET_ITEM(list, i);
             if (!exact_tensor(h)) return false;
             const Tensor& p = THPVariable_Unpack(h.ptr());
+            if (!p.is_same(q.params[i])) return false;
             const Tensor& g = p.grad();
             if (!g.defined()) continue;
             wtconv_dtype type;
@@ -605,8 +608,8 @@ void init(const std::vector<uintptr_t>& fns, py::object norm_py, py::object resi
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
 {
     py::class_<Group>(m, "AdamWGroup")
-        .def(py::init<std::vector<int64_t>, std::vector<int64_t>, std::vector<std::vector<int64_t>>, Tensor, Tensor,
-                      Tensor, OptTensor, OptTensor>());
+        .def(py::init<std::vector<Tensor>, std::vector<int64_t>, std::vector<int64_t>, std::vector<std::vector<int64_t>>,
+                      Tensor, Tensor, Tensor, OptTensor, OptTensor>());
     m.def("init", &init);
     m.def("layer_norm", &layer_norm);
     m.def("scaled_residual", &scaled_residual);

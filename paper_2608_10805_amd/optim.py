@@ -51,16 +51,16 @@ class AdamW(torch.optim.Optimizer):
     The moments are allocated with the group, in the order of the parameters' memory. `state[p]` holds views of them:
     "exp_avg" and "exp_avg_sq" (shaped as p with 32 bits; the codes, one an element in the order of memory, with 8),
     "exp_avg_scale", "exp_avg_sq_scale" and "order" (8 bits: which order that is, () or the strides), and "step", the
-    number of steps p has taken. A parameter without a gradient is left alone. Where a parameter's memory gets another
-    order (to channels_last, say), moments in 32 bits follow it; those in 8 bits share their scales in the old order,
-    so that a step is refused unless it is the first.
+    number of steps p has taken. A parameter without a gradient is left alone; a group's list of parameters stays as it
+    was added. Where a parameter's memory gets another order (to channels_last, say), moments in 32 bits follow it;
+    those in 8 bits share their scales in the old order, so that a step is refused unless it is the first.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, seed=0):
         if state_bits not in (8, 32):
             raise ValueError(f"state_bits must be 8 or 32, got {state_bits}")
         self.state_bits, self.seed = state_bits, int(seed)
-        self._buffers = []  # of each group: exp_avg, exp_avg_sq, their scales (8 bits), step, offsets, numel, orders
+        self._buffers = []  # of each group: exp_avg, exp_avg_sq, their scales (8 bits), step, params, offsets, numel, orders
         self._native = []   # the same for the native host path
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
 
@@ -99,7 +99,7 @@ class AdamW(torch.optim.Optimizer):
         buffers = {"exp_avg": new(end), "exp_avg_sq": new(end)}
         if coded:
             buffers.update(exp_avg_scale=new(end // block), exp_avg_sq_scale=new(end // block))
-        buffers.update(step=torch.zeros(len(params), dtype=torch.int64), offsets=offsets,
+        buffers.update(step=torch.zeros(len(params), dtype=torch.int64), params=list(params), offsets=offsets,
                        numel=[p.numel() for p in params], orders=[_order(p) for p in params])
         self._buffers.append(buffers)
         self._native.append(self._plan(params, buffers))
@@ -109,7 +109,8 @@ class AdamW(torch.optim.Optimizer):
     def _plan(self, params, buffers):
         """The group for the native host path, or None."""
         ext = autograd.load_block(params[0]) if params else False
-        return ext.AdamWGroup(*(buffers[n] for n in ("offsets", "numel", "orders", "step", "exp_avg", "exp_avg_sq")),
+        return ext.AdamWGroup(*(buffers[n] for n in ("params", "offsets", "numel", "orders", "step", "exp_avg",
+                                                      "exp_avg_sq")),
                               *(buffers.get(n) for n in ("exp_avg_scale", "exp_avg_sq_scale"))) if ext else None
 
     def _show(self, buffers, i, p):
@@ -164,6 +165,9 @@ class AdamW(torch.optim.Optimizer):
         device, taken, calls = None, [], {}  # calls: by the parameters' type, (groups, tensors)
         for index, (group, buffers) in enumerate(zip(self.param_groups, self._buffers)):
             lr, beta1, beta2, eps, decay = _hyperparameters(group)
+            if len(group["params"]) != len(buffers["params"]) or \
+                    any(p is not q for p, q in zip(group["params"], buffers["params"])):
+                raise ValueError(f"the parameters of group {index} are not those it was added with: add a group instead")
             places = {}  # of (type, step) in the call's groups
             steps = buffers["step"].tolist()
             for i, p in enumerate(group["params"]):
