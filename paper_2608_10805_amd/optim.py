@@ -26,8 +26,12 @@ def rounding_key(seed, step, group):
 
 def _strides_fill(t):
     """Whether the tensor's elements fill one run of memory, in any order of its dimensions."""
-    return t.is_contiguous() or (t.dim() == 4 and t.is_contiguous(memory_format=torch.channels_last)) or \
-        (t.dim() == 5 and t.is_contiguous(memory_format=torch.channels_last_3d))
+    run = 1
+    for stride, n in sorted((stride, n) for n, stride in zip(t.shape, t.stride()) if n != 1):
+        if stride != run:
+            return t.numel() == 0
+        run *= n
+    return True
 
 
 def _order(t):

@@ -6,6 +6,8 @@ import torch
 
 from paper_2608_10805_amd import autograd, optim
 
+from tests import _block as ref
+
 pytestmark = pytest.mark.gpu
 
 DEV = "cuda:0"
@@ -120,6 +122,29 @@ def test_a_reshaped_parameter_and_one_sided_dimensions_keep_their_order():
     r.data = r.data.to(memory_format=LAST)
     take(opt, [r], 1)
     assert int(opt.state[r]["step"]) == 2
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_parameters_in_any_dense_order(native, bits, monkeypatch):
+    """A transposed matrix fills its memory too."""
+    both_paths(monkeypatch, native)
+    base = torch.randn(70, 33, device=DEV)
+    turned, plain = torch.nn.Parameter(base.clone().t()), torch.nn.Parameter(base.clone())
+    cube = torch.nn.Parameter(torch.randn(5, 6, 7, device=DEV).permute(2, 0, 1))
+    a, b = optim.AdamW([turned, cube], lr=LR, state_bits=bits), optim.AdamW([plain], lr=LR, state_bits=bits)
+    assert not turned.is_contiguous() and not cube.is_contiguous()
+    for t in range(3):
+        plain.grad = some_grad(plain, t)
+        turned.grad = plain.grad.t().contiguous()  # brought into the parameter's order
+        cube.grad = some_grad(cube, t)
+        before = cube.detach().double().cpu()
+        a.step()
+        b.step()
+        assert torch.equal(turned.detach().t(), plain.detach())
+        if t == 0:
+            zero = torch.zeros(cube.shape, dtype=torch.float64)
+            ref.close(cube, ref.adamw(before, cube.grad.double().cpu(), zero, zero, 1, LR, (0.9, 0.999), 1e-8, 1e-2)[0], "f32", 8)
 
 
 # ----------------------------------------------------------------------------
