@@ -47,7 +47,12 @@ DEV void decode(uint32_t codes, int scale, float (&f)[kVec])
 }
 
 // The codes of four values under their block's scale: 20 mantissa bits are
-// dropped after `rest` was added to them. Zero under scale 255.
+// dropped after `rest` was added to them. Zero under scale 255. A second moment
+// that is not zero gets at least the first code: rounded to zero beside a first
+// moment that was rounded up, the next step would divide by the root of nearly
+// nothing (gradients of five decades in a block: updates of 700 times the rate,
+// now at most 1.8 times). The first code's root is the smallest step of m, in
+// units of their largest.
 template <bool SIGNED>
 DEV uint32_t encode(const float (&f)[kVec], int scale, const uint32_t (&rest)[kVec])
 {
@@ -55,7 +60,12 @@ DEV uint32_t encode(const float (&f)[kVec], int scale, const uint32_t (&rest)[kV
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
         c[i] = (__float_as_uint(__builtin_ldexpf(f[i], (SIGNED ? kMTop : kVTop) - scale)) + rest[i]) >> 20;
-        if (SIGNED) c[i] |= c[i] >> 4 & 0x80u;  // the sign, 11 bits up
+        if (SIGNED) {
+            c[i] |= c[i] >> 4 & 0x80u;  // the sign, 11 bits up
+        } else {
+            const uint32_t least = f[i] > 0.f;
+            c[i] = c[i] > least ? c[i] : least;
+        }
     }
     // the lowest bytes
     const uint32_t low = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u), high = __builtin_amdgcn_perm(c[3], c[2], 0x04000c0cu);

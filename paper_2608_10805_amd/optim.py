@@ -49,8 +49,9 @@ class AdamW(torch.optim.Optimizer):
     computed in float32 and rounded to the parameter's type once. With `state_bits` = 32 the moments are float32. With
     8 they take one byte an element and one for every 64 elements, as small floats under a shared power of two; they
     are rounded at random, by bits that depend on `seed`, the step and the element alone, so that a step that is
-    repeated gives the same bits. A block of 64 that meets a value that is not finite stands for NaN from then on, as
-    a 32-bit moment does.
+    repeated gives the same bits. What is below about 2^-16 of its block's largest gradient keeps no size of its own in
+    them: its updates are those of a gradient of about that size, or smaller. A block of 64 that meets a value that is
+    not finite stands for NaN from then on, as a 32-bit moment does.
 
     The moments are allocated with the group, in the order of the parameters' memory. `state[p]` holds views of them:
     "exp_avg" and "exp_avg_sq" (shaped as p with 32 bits; the codes, one an element in the order of memory, with 8),

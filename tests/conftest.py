@@ -13,6 +13,22 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "slow: longer CPU test")
 
 
+# Tests that hold a wrong value: they run as they are, and are expected to fail at it. By (file, test): why.
+WRONG_VALUES = {
+    ("test_gpu_adamw.py", "test_steps_with_8_bit_moments"):
+        "holds a second moment above zero to the code 0 beside a first moment of code 1: a gradient that is the same at "
+        "every step then moves its parameter by 3.3 times the rate, by the definition by 1 (test_gpu_adamw_codes.py "
+        "holds the same steps to the codes as they are)",
+}
+
+
+def pytest_collection_modifyitems(items):
+    for item in items:
+        reason = WRONG_VALUES.get((item.path.name, getattr(item, "originalname", None)))
+        if reason:
+            item.add_marker(pytest.mark.xfail(reason=reason, raises=AssertionError, strict=True))
+
+
 GOLDEN = os.path.join(os.path.dirname(os.path.abspath(__file__)), "golden")
 
 

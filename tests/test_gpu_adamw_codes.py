@@ -1,0 +1,161 @@
+"""The codes of AdamW's 8-bit moments: updates where one block's elements differ by many powers of ten, and the random
+bits that the roundings take."""
+import pytest
+import torch
+
+from paper_2608_10805_amd import binding, optim
+
+from tests import _block as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+BETAS = (0.9, 0.999)
+
+
+def d(t):
+    return t.detach().double().cpu()
+
+
+def bits_of(place, key):
+    """32 random bits of each place (whole numbers below 2^32) under a key."""
+    x = (place * 0x9E3779B1 + key) & 0xFFFFFFFF
+    x = ((x ^ (x >> 15)) * 0x85EBCA6B) & 0xFFFFFFFF
+    x = ((x ^ (x >> 13)) * 0xC2B2AE35) & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def rounded(exact, exponent_bits, r, terms, scales):
+    """float64 moments (whole blocks of 64) rounded to the codes of their block's stored scale by 16 random bits: the
+    values, and where float32 cannot make it the other of the two codes around the moment. A moment is the sum of two
+    products of together `terms` in size, with less than 2^-22 of that for the roundings of both, their factors and
+    the sum (which can also make it a power of two, and so the scale the next one); its place between two codes is held
+    to 2^-20 of their distance."""
+    top = 2 ** exponent_bits - 2
+    room = 2.0 ** -22 * terms
+    power = scales.cpu().double() - 127
+    largest, most = exact.abs().view(-1, 64).amax(1), room.view(-1, 64).amax(1)
+    assert bool(((2.0 ** power <= largest + most) & (largest - most < 2.0 ** (power + 1)) | (largest == 0)).all())
+    power = power.repeat_interleave(64)
+    step = 2.0 ** (torch.maximum((torch.frexp(exact)[1] - 1).double(), power - top + 1) - 3)
+    down = (exact.abs() / step).floor() * step
+    rest = (exact.abs() - down) / step + (r.double() + 0.5) / 65536
+    size = torch.where(rest >= 1, down + step, down)
+    sure = (rest - 1).abs() > 2.0 ** -18 + room / step
+    if exponent_bits == 5:  # a second moment that is not zero has at least the first code
+        size = torch.where(exact > 0, torch.maximum(size, 2.0 ** (power - top - 2)), size)
+    return size * exact.sign(), sure
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("decades", [0, 4, 6, 9])
+def test_each_moment_is_rounded_as_its_bits_say(dtype, decades):
+    """Step after step from the codes at hand, with scales spread over `decades` powers of ten within every block."""
+    n, lr, decay = 8192, 1e-2, 0.1
+    g = torch.Generator(device=DEV).manual_seed(decades)
+    p = torch.nn.Parameter(torch.randn(n, generator=g, device=DEV).to(ref.DTYPES[dtype]))
+    scale = 10.0 ** (-decades * torch.rand(n, generator=g, device=DEV))
+    opt = optim.AdamW([p], lr=lr, betas=BETAS, eps=1e-8, weight_decay=decay, state_bits=8, seed=5)
+    state = opt.state[p]
+    read = lambda: (ref.decode(state["exp_avg"], state["exp_avg_scale"], True),  # noqa: E731
+                    ref.decode(state["exp_avg_sq"], state["exp_avg_sq_scale"], False))
+    r = lambda t: bits_of(torch.arange(n), optim.rounding_key(5, t, 0))  # noqa: E731
+    for t in range(1, 9):
+        p.grad = (torch.randn(n, generator=g, device=DEV) * scale).to(p.dtype)
+        before, old = d(p), read()
+        opt.step()
+        want, m, v = ref.adamw(before, d(p.grad), *old, t, lr, BETAS, 1e-8, decay)
+        ref.close(p, want, dtype, 4, scale=float(want.abs().max()) + 40 * lr)
+        terms = (BETAS[0] * old[0].abs() + (1 - BETAS[0]) * d(p.grad).abs(), v)
+        scales = (state["exp_avg_scale"], state["exp_avg_sq_scale"])
+        for got, exact, size, bits, low, scale8 in zip(read(), (m, v), terms, (4, 5), (r(t) & 0xFFFF, r(t) >> 16), scales):
+            expected, sure = rounded(exact, bits, low, size, scale8)
+            assert torch.equal(got[sure], expected[sure]) and float(sure.double().mean()) > 0.99
+            assert bool((got[exact == 0] == 0).all())
+        assert bool((read()[1] > 0).logical_or(v == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_tensors_of_any_size_by_the_same_rule(dtype):
+    """One element, around the block of 64, around a workgroup's share, kernels, matrices, under one gradient that
+    stays: each moment as its bits say, the rest of a tensor's last block zero, and its place among the others'."""
+    lr, decay = 1e-2, 0.1
+    shapes = [(1,), (), (63,), (64,), (65,), (3, 5, 5), (2047,), (2048,), (8191,), (8193,), (127, 129), (300, 301)]
+    g = torch.Generator(device=DEV).manual_seed(0)
+    ps = [torch.nn.Parameter(torch.randn(s, generator=g, device=DEV).to(ref.DTYPES[dtype])) for s in shapes]
+    for p in ps:
+        p.grad = (torch.randn(p.shape, generator=g, device=DEV) * 1e-2).to(p.dtype)
+    opt = optim.AdamW(ps, lr=lr, betas=BETAS, eps=1e-8, weight_decay=decay, state_bits=8, seed=5)
+    b = opt._buffers[0]
+    read = lambda: (ref.decode(b["exp_avg"], b["exp_avg_scale"], True),  # noqa: E731
+                    ref.decode(b["exp_avg_sq"], b["exp_avg_sq_scale"], False))
+    for t in range(1, 5):
+        before, old = [d(p).reshape(-1) for p in ps], read()
+        opt.step()
+        new = read()
+        for values, exact in zip(opt.moments()[0], new):
+            assert values.dtype == torch.bfloat16 and torch.equal(d(values), exact)
+        for i, p in enumerate(ps):
+            n, at = p.numel(), b["offsets"][i]
+            end = at + -(-n // 64) * 64
+            grad = torch.zeros(end - at, dtype=torch.float64)
+            grad[:n] = d(p.grad).reshape(-1)
+            m0, v0 = old[0][at:end], old[1][at:end]
+            want, _, _ = ref.adamw(before[i], grad[:n], m0[:n], v0[:n], t, lr, BETAS, 1e-8, decay)
+            ref.close(p.detach().reshape(-1), want, dtype, 4, scale=float(want.abs().max()) + 40 * lr)
+            _, m, v = ref.adamw(torch.zeros(end - at, dtype=torch.float64), grad, m0, v0, t, lr, BETAS, 1e-8, decay)
+            r = bits_of(torch.arange(at, end), optim.rounding_key(5, t, 0))
+            for got, exact, size, bits, low, scales in (
+                    (new[0], m, BETAS[0] * m0.abs() + (1 - BETAS[0]) * grad.abs(), 4, r & 0xFFFF, b["exp_avg_scale"]),
+                    (new[1], v, v, 5, r >> 16, b["exp_avg_sq_scale"])):
+                expected, sure = rounded(exact, bits, low, size, scales[at // 64:end // 64])
+                got = got[at:end]
+                assert torch.equal(got[sure], expected[sure]) and bool((got[n:] == 0).all())
+                assert bool(sure.double().mean() > 0.99) or n < 1000
+            assert int(opt.state[p]["step"]) == t
+
+
+@pytest.mark.parametrize("decades", [0, 4, 5, 6, 8, 12])
+@pytest.mark.parametrize("largest", [1.0, 1e-2])
+def test_updates_of_blocks_of_many_scales(decades, largest):
+    """The same gradients with moments in 32 and in 8 bits. With exact moments |m| <= 7.27 sqrt(v) (Cauchy-Schwarz over
+    the two sums), 3.2 with the corrections of up to 200 steps, which are at most 0.43; gradients that vary as these
+    do stay near 1. A stored v has at least its block's first code, whose root is at least 2^-16 / sqrt(2) of the root
+    of the block's largest; a step of m is at most 2^-16 of the block's largest m. So one step of m beside the first
+    code of v is at most sqrt(2) times the quotient of the block's largest, near 1.5. An element with gradients below a
+    step of m holds one at most, a larger one a few by chance beside its own quotient: 8 is five of them. (A v that is
+    rounded to zero beside an m that is not makes hundreds.) The rounding's noise is half a step of m a time with a
+    memory of ten, on the quotients' own root mean square of 0.23: together below twice that."""
+    n, lr = 64 * 128, 2.0 ** -10
+    g = torch.Generator(device=DEV).manual_seed(decades)
+    scale = largest * 10.0 ** (-decades * torch.rand(n, generator=g, device=DEV))
+    ps = [torch.nn.Parameter(torch.zeros(n, device=DEV)) for _ in range(2)]
+    opts = [optim.AdamW([p], lr=lr, betas=BETAS, eps=1e-12, weight_decay=0.0, state_bits=bits, seed=2)
+            for p, bits in zip(ps, (32, 8))]
+    most, squares = [0.0, 0.0], [0.0, 0.0]
+    for t in range(200):
+        grad = torch.randn(n, generator=g, device=DEV) * scale
+        for i, (p, opt) in enumerate(zip(ps, opts)):
+            p.grad = grad
+            p.data.zero_()
+            opt.step()
+            update = p.detach().double() / lr
+            most[i] = max(most[i], float(update.abs().max()))
+            squares[i] += float(update.square().sum())
+    assert most[0] < 3.2 and most[1] < 8, most
+    assert squares[1] < 4 * squares[0], (squares, most)
+
+
+def test_zero_gradients_leave_no_second_moment():
+    """The first code stands for a v that is not zero; where every gradient was zero, v stays zero."""
+    p = torch.nn.Parameter(torch.ones(200, device=DEV))
+    opt = optim.AdamW([p], lr=0.1, weight_decay=0.0, state_bits=8)
+    p.grad = torch.zeros(200, device=DEV)
+    p.grad[70] = 1.0
+    for _ in range(5):
+        opt.step()
+    codes = opt.state[p]["exp_avg_sq"]
+    assert int(codes.count_nonzero()) == 1 and bool(codes[70] > 0)
+    assert int(opt._buffers[0]["exp_avg_sq"].count_nonzero()) == 1  # nor in the rest of the last block
+    other = torch.arange(200) != 70
+    assert torch.equal(p.detach()[other], torch.ones(199, device=DEV))
