@@ -114,10 +114,17 @@ DEV float divided(float s, float n, float per)
 
 // 1 / sqrt(v), the hardware's approximation and one Newton step. Every lane of a
 // pixel computes it, so the library's exact steps would cost more than the sums.
+// The hardware takes a subnormal v for zero, so small ones are scaled first; at
+// zero and infinity (a variance that overflowed) the approximation is exact and
+// the step would make it NaN.
 DEV float inverse_root(float v)
 {
-    const float r = __builtin_amdgcn_rsqf(v);
-    return __builtin_fmaf(0.5f * __builtin_fmaf(-v * r, r, 1.0f), r, r);
+    const bool small = v < 0x1p-96f;
+    const float u = small ? v * 0x1p64f : v;
+    const float r = __builtin_amdgcn_rsqf(u);
+    const float n = __builtin_fmaf(0.5f * __builtin_fmaf(-u * r, r, 1.0f), r, r);
+    const float root = u > 0.f && u < __builtin_inff() ? n : r;
+    return small ? root * 0x1p32f : root;
 }
 
 inline int at_most(int64_t items, int64_t most) { return (int)(items < most ? (items > 1 ? items : 1) : most); }
