@@ -69,6 +69,25 @@ class AdamW(torch.optim.Optimizer):
         self._native = []   # the same for the native host path
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
 
+    def __getstate__(self):
+        return {**super().__getstate__(), "state_bits": self.state_bits, "seed": self.seed}
+
+    def __setstate__(self, state):
+        """A copy: its groups' buffers are allocated anew and take the moments and steps over."""
+        super().__setstate__(state)
+        self._buffers, self._native = [], []
+        for group in self.param_groups:
+            held = [self.state[p] for p in group["params"]]
+            self._allocate(group)
+            buffers = self._buffers[-1]
+            for i, (p, old) in enumerate(zip(group["params"], held)):
+                for k, t in self.state[p].items():
+                    if k == "order":  # (not p's, where that changed since the last step)
+                        self.state[p][k] = buffers["orders"][i] = old[k]
+                    else:
+                        t.copy_(old[k])
+            self._native[-1] = self._plan(group["params"], buffers)
+
     def add_param_group(self, param_group):
         super().add_param_group(param_group)
         group = self.param_groups[-1]

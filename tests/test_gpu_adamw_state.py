@@ -1,4 +1,7 @@
 """AdamW as a program keeps it: its groups, copies and saved states."""
+import copy
+import pickle
+
 import pytest
 import torch
 
@@ -8,6 +11,7 @@ pytestmark = pytest.mark.gpu
 
 DEV = "cuda:0"
 LR = 1e-2
+LAST = torch.channels_last
 
 
 def image_kernel(seed=0, shape=(8, 6, 3, 3), dtype=torch.float32):
@@ -51,3 +55,42 @@ def test_parameters_of_a_changed_group_are_refused(native, monkeypatch):
     group["params"] = list(ps)
     opt.step()
     assert [int(opt.state[p]["step"]) for p in ps] == [2, 2, 2]
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("how", ["deepcopy", "pickle"])
+def test_copies_of_an_optimizer_go_on_by_themselves(bits, how):
+    """A copy has parameters, moments, steps and a seed of its own, and steps as the first one does."""
+    ps = [image_kernel(), image_kernel(1, (70, 9), torch.bfloat16), image_kernel(2, (1,))]
+    ps[0].data = ps[0].data.to(memory_format=LAST)
+    opt = optim.AdamW([{"params": ps[:1], "lr": 0.1}, {"params": ps[1:]}], lr=LR, state_bits=bits, seed=6)
+    take(opt, ps, 0)
+    other = copy.deepcopy(opt) if how == "deepcopy" else pickle.loads(pickle.dumps(opt))
+    qs = [p for g in other.param_groups for p in g["params"]]
+    kept = [q.detach().clone() for q in qs]
+    assert all(torch.equal(p.detach(), q) for p, q in zip(ps, kept))
+    take(opt, ps, 1)
+    assert all(torch.equal(q.detach(), k) for q, k in zip(qs, kept))  # its own memory
+    assert all(int(other.state[q]["step"]) == 1 for q in qs)
+    take(other, qs, 1)
+    assert all(torch.equal(p.detach(), q.detach()) for p, q in zip(ps, qs))
+    assert all(torch.equal(a, b) for x, y in zip(opt.moments(), other.moments()) for a, b in zip(x, y))
+    assert other.param_groups[0]["lr"] == 0.1 and other.state_bits == bits and other.seed == 6
+    other.add_param_group({"params": [image_kernel(3)]})
+    other.load_state_dict(copy.deepcopy(other.state_dict()))
+
+
+def test_a_copy_keeps_the_order_that_8_bit_moments_are_in():
+    """Also where a parameter has left it since the last step: both optimizers refuse the next one."""
+    p = image_kernel()
+    opt = optim.AdamW([p], lr=LR, state_bits=8)
+    take(opt, [p], 0)
+    p.data = p.data.to(memory_format=LAST)
+    other = copy.deepcopy(opt)
+    q = other.param_groups[0]["params"][0]
+    for o, t in ((opt, p), (other, q)):
+        with pytest.raises(ValueError, match="order"):
+            take(o, [t], 1)
+        t.data = t.data.contiguous()
+        take(o, [t], 1)
+    assert torch.equal(p.detach(), q.detach())
