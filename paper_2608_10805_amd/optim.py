@@ -242,9 +242,13 @@ class AdamW(torch.optim.Optimizer):
                 binding.adamw_moments(b["exp_avg"], b["exp_avg_scale"], b["exp_avg_sq"], b["exp_avg_sq_scale"], dtype)
                 for b, native in zip(self._buffers, self._native)]
 
+    def state_dict(self):
+        """The moments and hyperparameters as torch's optimizers give them, and the seed."""
+        return {**super().state_dict(), "seed": self.seed}
+
     def load_state_dict(self, state_dict):
-        """Copy the hyperparameters and the moments of a state_dict() of an optimizer with the same groups, shapes and
-        state_bits into this one."""
+        """Copy the hyperparameters, the moments and the seed (if it is there) of a state_dict() of an optimizer with
+        the same groups, shapes and state_bits into this one."""
         saved, groups = state_dict["state"], state_dict["param_groups"]
         if [len(g["params"]) for g in groups] != [len(g["params"]) for g in self.param_groups]:
             raise ValueError("the state has other parameter groups")
@@ -269,6 +273,7 @@ class AdamW(torch.optim.Optimizer):
                     t.copy_(state[k])
         for ours, g in zip(self.param_groups, groups):
             ours.update({k: v for k, v in g.items() if k != "params"})
+        self.seed = int(state_dict.get("seed", self.seed))
 
 
 def _gradient(p, buffers, i):

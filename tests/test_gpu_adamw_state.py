@@ -94,3 +94,19 @@ def test_a_copy_keeps_the_order_that_8_bit_moments_are_in():
         t.data = t.data.contiguous()
         take(o, [t], 1)
     assert torch.equal(p.detach(), q.detach())
+
+
+def test_a_resumed_run_rounds_as_the_first_one_would_have(tmp_path):
+    """The seed is part of the state, also through a file that is read without running anything from it."""
+    p = image_kernel()
+    opt = optim.AdamW([p], lr=LR, state_bits=8, seed=11)
+    take(opt, [p], 0)
+    torch.save(opt.state_dict(), tmp_path / "state.pt")
+    q = torch.nn.Parameter(p.detach().clone())
+    other = optim.AdamW([q], lr=0.5, state_bits=8, seed=12)
+    other.load_state_dict(torch.load(tmp_path / "state.pt", weights_only=True))
+    for t in (1, 2):
+        take(opt, [p], t)
+        take(other, [q], t)
+    assert torch.equal(p.detach(), q.detach())
+    assert all(torch.equal(a, b) for a, b in zip(opt.moments()[0], other.moments()[0]))
