@@ -249,6 +249,9 @@ class AdamW(torch.optim.Optimizer):
     def load_state_dict(self, state_dict):
         """Copy the hyperparameters, the moments and the seed (if it is there) of a state_dict() of an optimizer with
         the same groups, shapes and state_bits into this one."""
+        for hook in self._optimizer_load_state_dict_pre_hooks.values():
+            changed = hook(self, state_dict)
+            state_dict = state_dict if changed is None else changed
         saved, groups = state_dict["state"], state_dict["param_groups"]
         if [len(g["params"]) for g in groups] != [len(g["params"]) for g in self.param_groups]:
             raise ValueError("the state has other parameter groups")
@@ -274,6 +277,8 @@ class AdamW(torch.optim.Optimizer):
         for ours, g in zip(self.param_groups, groups):
             ours.update({k: v for k, v in g.items() if k != "params"})
         self.seed = int(state_dict.get("seed", self.seed))
+        for hook in self._optimizer_load_state_dict_post_hooks.values():
+            hook(self)
 
 
 def _gradient(p, buffers, i):

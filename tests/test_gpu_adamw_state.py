@@ -110,3 +110,24 @@ def test_a_resumed_run_rounds_as_the_first_one_would_have(tmp_path):
         take(other, [q], t)
     assert torch.equal(p.detach(), q.detach())
     assert all(torch.equal(a, b) for a, b in zip(opt.moments()[0], other.moments()[0]))
+
+
+def test_hooks_around_loading_a_state():
+    p, q = image_kernel(), image_kernel()
+    a, b = (optim.AdamW([t], lr=LR) for t in (p, q))
+    take(a, [p], 0)
+    seen = []
+
+    def before(opt, state):
+        seen.append("before")
+        assert opt is b and int(b.state[q]["step"]) == 0
+        return {**state, "param_groups": [{**g, "lr": 0.25} for g in state["param_groups"]]}
+
+    def after(opt):
+        seen.append("after")
+        assert opt is b and int(b.state[q]["step"]) == 1
+
+    b.register_load_state_dict_pre_hook(before)
+    b.register_load_state_dict_post_hook(after)
+    b.load_state_dict(copy.deepcopy(a.state_dict()))
+    assert seen == ["before", "after"] and b.param_groups[0]["lr"] == 0.25 and a.param_groups[0]["lr"] == LR
