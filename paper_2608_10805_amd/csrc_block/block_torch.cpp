@@ -492,9 +492,9 @@ struct Call {
     std::vector<wtconv_adamw_tensor> tensors;
 };
 
-// One step of every parameter that has a gradient. hyper: (lr, beta1, beta2,
-// eps, weight_decay) of each group. False, with nothing done, where one of them
-// is not the plain case.
+// One step of every parameter that has a gradient. plans: null for a group of no
+// parameters. hyper: (lr, beta1, beta2, eps, weight_decay) of each group. False,
+// with nothing done, where one of them is not the plain case.
 bool adamw_step(const std::vector<Group*>& plans, py::sequence params, const std::vector<std::array<double, 5>>& hyper,
                 int bits, uint64_t seed, py::handle scale)
 {
@@ -503,8 +503,10 @@ bool adamw_step(const std::vector<Group*>& plans, py::sequence params, const std
     std::vector<std::pair<int64_t*, const Tensor*>> taken;
     std::optional<c10::Device> dev;
     for (size_t gi = 0; gi < plans.size(); ++gi) {
-        const Group& q = *plans[gi];
         PyObject* list = params[gi].ptr();
+        if (!plans[gi] && PyList_CheckExact(list) && PyList_GET_SIZE(list) == 0) continue;
+        if (!plans[gi]) return false;
+        const Group& q = *plans[gi];
         if (!PyList_CheckExact(list) || (size_t)PyList_GET_SIZE(list) != q.numel.size()) return false;
         int64_t* steps = q.steps.mutable_data_ptr<int64_t>();
         int64_t place_step[3] = {-1, -1, -1};  // the step of the call's last group, if it is of this parameter group

@@ -131,7 +131,7 @@ class AdamW(torch.optim.Optimizer):
             self._show(buffers, i, p)
 
     def _plan(self, params, buffers):
-        """The group for the native host path, or None."""
+        """The group for the native host path; None without it, and for no parameters."""
         ext = autograd.load_block(params[0]) if params else False
         return ext.AdamWGroup(*(buffers[n] for n in ("params", "offsets", "numel", "orders", "step", "exp_avg",
                                                       "exp_avg_sq")),
@@ -177,7 +177,7 @@ class AdamW(torch.optim.Optimizer):
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("an AdamW step cannot be captured: the bias corrections of its step would be replayed")
         ext = autograd._block
-        if not (ext and all(self._native) and
+        if not (ext and all(native or not g["params"] for native, g in zip(self._native, self.param_groups)) and
                 ext.adamw_step(self._native, [g["params"] for g in self.param_groups],
                                [_hyperparameters(g) for g in self.param_groups], self.state_bits, self.seed & _M32,
                                grad_scale)):
@@ -240,6 +240,7 @@ class AdamW(torch.optim.Optimizer):
         ext = autograd._block
         return [ext and native and ext.adamw_moments(native, dtype) or
                 binding.adamw_moments(b["exp_avg"], b["exp_avg_scale"], b["exp_avg_sq"], b["exp_avg_sq_scale"], dtype)
+                if b["params"] else (b["exp_avg"].to(dtype), b["exp_avg_sq"].to(dtype))
                 for b, native in zip(self._buffers, self._native)]
 
     def state_dict(self):

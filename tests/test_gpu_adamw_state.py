@@ -131,3 +131,23 @@ def test_hooks_around_loading_a_state():
     b.register_load_state_dict_post_hook(after)
     b.load_state_dict(copy.deepcopy(a.state_dict()))
     assert seen == ["before", "after"] and b.param_groups[0]["lr"] == 0.25 and a.param_groups[0]["lr"] == LR
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_an_empty_group_stays_on_the_native_path(bits, monkeypatch):
+    """It neither sends the others through Python nor changes their random bits, and its moments are empty."""
+    runs = []
+    for native in (True, False):
+        ps = [image_kernel(), image_kernel(1)]
+        opt = optim.AdamW([{"params": ps[:1]}, {"params": []}, {"params": ps[1:]}], lr=LR, state_bits=bits)
+        if native:
+            monkeypatch.setattr(opt, "_step", lambda scale: pytest.fail("left to Python"))
+        else:
+            opt._native = [None] * 3
+        take(opt, ps, 0)
+        take(opt, ps, 1)
+        m, v = opt.moments()[1]
+        assert m.numel() == v.numel() == 0
+        assert m.dtype == v.dtype == (torch.bfloat16 if bits == 8 else torch.float32)
+        runs.append([p.detach().clone() for p in ps])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
