@@ -524,6 +524,8 @@ bool adamw_step(const std::vector<Group*>& plans, py::sequence params, const std
                 return false;
             if (dev && *dev != p.device()) return false;
             dev = p.device();
+            taken.emplace_back(steps + i, &p);
+            if (!q.numel[i]) continue;  // (a group of nothing else has no buffers)
             Call& c = calls[type];
             const int64_t step = steps[i] + 1;
             if (place_step[type] != step) {
@@ -541,7 +543,6 @@ bool adamw_step(const std::vector<Group*>& plans, py::sequence params, const std
             }
             c.tensors.push_back({p.mutable_data_ptr(), g.const_data_ptr(), q.numel[i], q.offsets[i],
                                  (int)c.groups.size() - 1});
-            taken.emplace_back(steps + i, &p);
         }
     }
     if (!dev) return true;

@@ -201,6 +201,9 @@ class AdamW(torch.optim.Optimizer):
                 if _order(p) != buffers["orders"][i]:
                     self._reorder(index, i, p)
                 device, step = p.device, steps[i] + 1
+                taken.append((buffers["step"], i, p, grad))  # a gradient that was copied lives until the launch
+                if not p.numel():  # (a group of nothing else has no buffers)
+                    continue
                 code = binding._dtype_code(p)
                 groups, tensors = calls.setdefault(code, ([], []))
                 if (code, step) not in places:
@@ -213,7 +216,6 @@ class AdamW(torch.optim.Optimizer):
                                                      *scales))
                 tensors.append(binding.AdamWTensor(p.data_ptr(), grad.data_ptr(), p.numel(), buffers["offsets"][i],
                                                    places[code, step]))
-                taken.append((buffers["step"], i, p, grad))  # a gradient that was copied lives until the launch
         if device is None:
             return
         if grad_scale is not None:

@@ -151,3 +151,19 @@ def test_an_empty_group_stays_on_the_native_path(bits, monkeypatch):
         assert m.dtype == v.dtype == (torch.bfloat16 if bits == 8 else torch.float32)
         runs.append([p.detach().clone() for p in ps])
     assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_parameters_of_no_elements(native, bits, monkeypatch):
+    """By themselves and beside others, with gradients."""
+    both_paths(monkeypatch, native)
+    none, some = torch.nn.Parameter(torch.empty(0, 3, device=DEV)), image_kernel()
+    alone = optim.AdamW([none], state_bits=bits)
+    mixed = optim.AdamW([{"params": [none]}, {"params": [some, none.detach()]}], state_bits=bits)
+    none.grad = torch.empty(0, 3, device=DEV)
+    alone.step()
+    assert int(alone.state[none]["step"]) == 1
+    kept = some.detach().clone()
+    take(mixed, [some], 0)
+    assert not torch.equal(some.detach(), kept)
