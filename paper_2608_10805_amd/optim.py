@@ -94,8 +94,11 @@ class AdamW(torch.optim.Optimizer):
         try:
             self._check_group(group)
             self._allocate(group)
-        except ValueError:
+        except BaseException:  # (an argument, or no memory for the moments)
             self.param_groups.pop()
+            del self._buffers[len(self.param_groups):], self._native[len(self.param_groups):]
+            for p in group["params"]:
+                self.state.pop(p, None)
             raise
 
     def _check_group(self, group):

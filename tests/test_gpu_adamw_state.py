@@ -167,3 +167,18 @@ def test_parameters_of_no_elements(native, bits, monkeypatch):
     kept = some.detach().clone()
     take(mixed, [some], 0)
     assert not torch.equal(some.detach(), kept)
+
+
+def test_a_group_that_cannot_be_added_is_not_there():
+    """Whatever was wrong with it."""
+    p = image_kernel()
+    opt = optim.AdamW([p], lr=LR)
+    for bad, error in (({"params": [image_kernel(1)], "lr": None}, TypeError),
+                       ({"params": [image_kernel(2)], "betas": 0.9}, TypeError),
+                       ({"params": [image_kernel(3)], "eps": -1.0}, ValueError)):
+        with pytest.raises(error):
+            opt.add_param_group(bad)
+        assert len(opt.param_groups) == len(opt._buffers) == len(opt._native) == 1
+    take(opt, [p], 0)
+    opt.add_param_group({"params": [image_kernel(4)]})
+    assert len(opt.param_groups) == len(opt._buffers) == 2
