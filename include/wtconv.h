@@ -364,7 +364,8 @@ wtconv_status wtconv_scaled_residual_backward(const wtconv_residual_desc* desc, 
  * less than half the distance between two codes, so that rounding to nearest
  * would hold v where it is): 20 mantissa bits are dropped after 16 * r + 8 was
  * added, with the low 16 bits r of a hash of `key` and of the element's place
- * in the buffer for m, and the high 16 bits for v. A v > 0 gets code 1 where this
+ * in the buffer for m, and the high 16 bits for v (of a place from 2^32 on: of
+ * its low 32 bits, under a key that is the hash of `key` and of its high ones). A v > 0 gets code 1 where this
  * rounds it to 0: it is less than 2^-31 of its block's largest then, and beside an
  * m that was rounded up a v of 0 would make the next update far too large. The
  * update of p takes the moments before this rounding.

@@ -21,7 +21,9 @@ constexpr int kThreads = 256, kVec = 4;
 constexpr int kChunk = 2 * kThreads * kVec;  // elements of one workgroup
 constexpr int kMTop = 14, kVTop = 30;        // exponent field of a block's largest moment
 
-// 32 random bits for an element's place under a key.
+// 32 random bits for an element's place under a key: a golden-ratio step from
+// place to place (2^32 / 1.618, as a prime), then the shifts and multipliers of
+// a published 32-bit hash's last mixing (A. Appleby, public domain).
 DEV uint32_t random_bits(uint32_t place, uint32_t key)
 {
     uint32_t x = place * 0x9E3779B1u + key;
@@ -121,7 +123,6 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamArgs a)
     M *hm = (M*)h.m + at0, *hv = (M*)h.v + at0;
     uint8_t *hms = h.ms + (at0 >> 6), *hvs = h.vs + (at0 >> 6);
     const float gscale = a.scale ? *a.scale : 1.0f;
-    const uint32_t key = h.key + (uint32_t)((uint64_t)at0 >> 32) * 0x9E3779B1u;  // (a chunk does not cross 2^32: both are multiples of 64)
     const int end = n - e0 < kChunk ? (int)(n - e0) : kChunk;
     // (lanes of one block of 64 elements go on or stop together; past a tensor's
     // end its last block has zeros, which stay zeros)
@@ -175,9 +176,12 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamArgs a)
         if constexpr (CODED) {
             const int ms = block_scale<true>(m), vs = block_scale<false>(v);
             uint32_t rm[kVec], rv[kVec];
+            // from the 2^32nd place on, which four places side by side do not cross, under a key of their own
+            const uint64_t place = (uint64_t)at0 + c;
+            const uint32_t high = (uint32_t)(place >> 32), key = high ? random_bits(high, h.key) : h.key;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const uint32_t r = random_bits((uint32_t)at0 + c + i, key);
+                const uint32_t r = random_bits((uint32_t)place + i, key);
                 rm[i] = (r << 4 & 0xffff0u) | 8;
                 rv[i] = (r >> 12 & 0xffff0u) | 8;
             }

@@ -159,3 +159,37 @@ def test_zero_gradients_leave_no_second_moment():
     assert int(opt._buffers[0]["exp_avg_sq"].count_nonzero()) == 1  # nor in the rest of the last block
     other = torch.arange(200) != 70
     assert torch.equal(p.detach()[other], torch.ones(199, device=DEV))
+
+
+def test_random_bits_of_places_around_2_32():
+    """A tensor from the block before the 2^32nd element on: every element's bits are those of its own place, which
+    from there on are taken under a key of their own."""
+    first, n = (1 << 32) - 64, 5000
+    end = first + -(-n // 64) * 64
+    new = lambda k: torch.zeros(k, dtype=torch.uint8, device=DEV)  # noqa: E731
+    m, v, ms, vs = new(end), new(end), new(end // 64), new(end // 64)
+    g = torch.Generator(device=DEV).manual_seed(0)
+    p, grad = torch.zeros(n, device=DEV), torch.randn(n, generator=g, device=DEV)
+    key = optim.rounding_key(3, 1, 0)
+    group = binding.AdamWGroup(0.1, *BETAS, 1e-8, 0.0, 1, key, *(t.data_ptr() for t in (m, v, ms, vs)))
+    tensor = binding.AdamWTensor(p.data_ptr(), grad.data_ptr(), n, first, 0)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert binding.wtconv_adamw_step([group], [tensor], 0, 8, None, stream) == 0
+    place = torch.arange(first, end)
+    high = place >> 32
+    assert int(high[0]) == 0 and int(high[-1]) == 1
+    keys = torch.where(high > 0, bits_of(high, key), key)
+    r = bits_of(place & 0xFFFFFFFF, keys)
+    exact = torch.zeros(end - first, dtype=torch.float64)
+    exact[:n] = d(grad)
+    for codes, scales, value, bits, low in ((m, ms, exact * (1 - BETAS[0]), 4, r & 0xFFFF),
+                                            (v, vs, exact * exact * (1 - BETAS[1]), 5, r >> 16)):
+        got = ref.decode(codes[first:end], scales[first // 64:], bits == 4)
+        want, sure = rounded(value, bits, low, value.abs(), scales[first // 64:])
+        assert torch.equal(got[sure], want[sure]) and float(sure.double().mean()) > 0.99
+    # the places after 2^32 do not take the bits of those from 0 on, nor of their neighbours there
+    for shift in (0, 1):
+        other = bits_of((place & 0xFFFFFFFF) + shift, key)
+        assert float((r == other)[high > 0].double().mean()) < 0.01
+    assert int(m[:first].count_nonzero()) == 0 and bool(p.isfinite().all())
+    torch.cuda.empty_cache()
