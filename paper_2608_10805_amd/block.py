@@ -16,7 +16,8 @@ from .autograd import LayerNorm, WTConv2d, scaled_residual
 
 class WTConvNeXtBlock(torch.nn.Module):
     """x [B, C, H, W] -> the same shape and type. The convolution's, norm's and layer scale's parameters are float32;
-    the products run in x's type. `drop_path` is the probability that training drops an image's branch."""
+    the products run in x's type, or in autocast's. `drop_path` is the probability that training drops an image's
+    branch."""
 
     def __init__(self, channels, kernel_size=5, levels=3, hidden=None, layer_scale=1e-6, drop_path=0.0, device=None):
         super().__init__()
@@ -39,7 +40,7 @@ class WTConvNeXtBlock(torch.nn.Module):
         keep = None
         if self.training and self.drop_path:
             keep = (torch.rand(x.shape[0], device=x.device) >= self.drop_path).float() / (1 - self.drop_path)
-        return scaled_residual(x, z, self.gamma, keep)
+        return scaled_residual(x, z.to(x.dtype), self.gamma, keep)  # (autocast's products are in its type)
 
 
 class WTConvNeXt(torch.nn.Module):
