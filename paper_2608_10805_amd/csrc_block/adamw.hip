@@ -8,10 +8,11 @@
 // and others four.
 //
 // Bound by memory with 32-bit moments: 39 million float32 elements 206 us, 5.3
-// TB/s of 28 bytes an element, what a large copy reaches. With 8-bit moments
-// (16.06 bytes) 20 million float32 elements take 66 us, 4.9 TB/s; bfloat16
-// parameters (10.06 bytes) 54 us, 3.7 TB/s, bound by the arithmetic of the codes
-// (281 vector instructions for four elements).
+// TB/s of 28 bytes an element, what a large copy reaches; 20 million bfloat16 ones
+// 90 us, 4.9 TB/s of 22 bytes. With 8-bit moments (16.06 bytes) 20 million float32
+// elements take 64 us, 5.0 TB/s; bfloat16 parameters (10.06 bytes) 51 to 59 us, 3.4
+// to 3.9 TB/s, bound by the arithmetic of the codes (303 vector instructions in the
+// loop over four elements, the branches that few take among them).
 #include "norm_device.h"
 
 namespace wtc {

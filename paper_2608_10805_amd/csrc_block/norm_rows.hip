@@ -7,10 +7,12 @@
 // and rows may begin at any element.
 //
 // Bound by memory where many rows are on their way (191520 rows of 96 float32
-// channels: forward 34 us, 4.3 TB/s, backward 49 us, 4.5 TB/s); in 16 bits the
-// sums over lanes and the conversions show (the same rows in bfloat16 23.7 us,
-// 3.1 TB/s, and 37 us, 3.0 TB/s; 47880 rows of 127 float16 channels 10.6 and
-// 15.4 us, 2.3 TB/s).
+// channels: forward 34 us, 4.3 TB/s, backward 49 us, 4.5 TB/s). In 16 bits the
+// latency of a row shows: a group of the forward pass takes one row, loads the
+// weight and the bias after its sums and has nothing on its way meanwhile, and
+// the sums over lanes and the conversions are as many as for twice the bytes (the
+// same rows in bfloat16 23.7 us, 3.1 TB/s, and 37 us, 3.0 TB/s; 47880 rows of 127
+// float16 channels 10.4 and 15.2 us, 2.3 TB/s, with incomplete vectors besides).
 #include "norm_device.h"
 
 namespace wtc {

@@ -56,9 +56,10 @@ class AdamW(torch.optim.Optimizer):
     The moments are allocated with the group, in the order of the parameters' memory. `state[p]` holds views of them:
     "exp_avg" and "exp_avg_sq" (shaped as p with 32 bits; the codes, one an element in the order of memory, with 8),
     "exp_avg_scale", "exp_avg_sq_scale" and "order" (8 bits: which order that is, () or the strides), and "step", the
-    number of steps p has taken. A parameter without a gradient is left alone; a group's list of parameters stays as it
-    was added. Where a parameter's memory gets another order (to channels_last, say), moments in 32 bits follow it;
-    those in 8 bits share their scales in the old order, so that a step is refused unless it is the first.
+    number of steps p has taken; they are changed by writing into the views. A parameter without a gradient is left
+    alone; a group's list of parameters stays as it was added. Where a parameter's memory gets another order (to
+    channels_last, say), moments in 32 bits follow it; those in 8 bits share their scales in the old order, so that a
+    step is refused unless it is the first.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, seed=0):
